@@ -179,7 +179,7 @@ def prepare(case, seed):
 def _plain_codes(v, top):
     """int8 codes of the rows of v (fp32) whose largest magnitudes are `top`."""
     live = (top >= TINY) & torch.isfinite(top)
-    inv = torch.where(live, 127.0 / top, torch.zeros_like(top))
+    inv = torch.where(live, torch.full_like(top, 127.0).div(top), torch.zeros_like(top))
     return torch.where(live[:, None], torch.round(v * inv[:, None]), torch.zeros_like(v))
 
 
@@ -335,7 +335,7 @@ def _codes64(v32):
     a = torch.max(torch.abs(v32), dim=1)[0]
     c = torch.zeros_like(v32)
     full = (a >= TINY).nonzero()[:, 0]
-    c[full] = torch.clamp(torch.round(v32[full] * (127.0 / a[full]).unsqueeze(1)), -127, 127)
+    c[full] = torch.clamp(torch.round(v32[full] * torch.true_divide(torch.full_like(a[full], 127.0), a[full]).unsqueeze(1)), -127, 127)
     return c.double(), a
 
 
