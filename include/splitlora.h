@@ -343,6 +343,62 @@ int splitlora_handoff_quantize(int dtype, const void* x, int64_t M, int d, uint8
                                void* stream);
 int splitlora_handoff_dequantize(int dtype, const uint8_t* codes, const float* scales, int64_t M, int d,
                                  void* y, void* stream);
+/* ---- adapters over a frozen weight held in 8 bits ----
+ * Rows in 8 bits: int8 codes and one fp32 scale per row; a row of activations or gradients is a token, a row of a weight
+ * [out, in] an output channel.  The calls below take any sizes in the limits given and any alignment of an element;
+ * 16-byte aligned rows are the fast ones.  M: rows, 1 <= M < 2^31.  ld_codes, ld_x, ld_w: bytes between two rows of codes, at
+ * least the row's width; multiples of 16 (with 16-byte aligned bases) let the product run on the tensor cores.  Bytes
+ * between a row's codes and the next row are neither read into a result nor written.
+ *
+ * _quantize_rows: with v = x[m,c] * col_scale[c] (col_scale [d] fp32 or NULL: v = x) and a = max_c |v|, in fp32,
+ *   codes[m,c] = v * (127 / a) rounded to the nearest integer, ties to even;  scales[m] = a / 127.
+ * A row whose a is below 1e-36 has scale 0 and codes 0; a row that holds an inf or NaN has scale NaN and codes 0.  col_scale is how
+ * the channel scales of a weight enter the gradient of its input: dx = (dy o w_scales) Wq, with Wq^T [in, out] as
+ * the weight of splitlora_linear_i8 and no w_scales there.  1 <= d <= 65536.
+ * _dequantize_rows: y[m,c] = codes[m,c] * scales[m], rounded once to `dtype`. */
+int splitlora_quantize_rows(int dtype, const void* x, const float* col_scale, int64_t M, int d, int8_t* codes,
+                            int64_t ld_codes, float* scales, void* stream);
+int splitlora_dequantize_rows(int dtype, const int8_t* codes, int64_t ld_codes, const float* scales, int64_t M, int d,
+                              void* y, void* stream);
+/* RMSNorm of a residual stream with an int8 output.  With s = x + residual (residual NULL: s = x), fp32:
+ *   rstd = (mean_c s^2 + eps)^-1/2 ;  v = s g ;  codes and a as above ;  scales[m] = a rstd / 127
+ *   h = s (NULL: not written) and y = v rstd (NULL: not written), each rounded once to `dtype`.
+ * x, residual, h, y [M, d], g [d] in `dtype`, contiguous; h may be x or residual.  1 <= d <= 16384, eps >= 0.  A row that
+ * holds an inf or NaN has scale NaN and codes 0.
+ * _bwd: the gradient with respect to s (which is that of x and of residual) from dy, the gradient of the normalised row (the rounding
+ * to codes passes it on unchanged), and h as stored:
+ *   w = dy g ;  dx = residual + rstd (w - h rstd^2 mean_c(w h)) ;  dg_c = sum_m dy h rstd
+ * residual: the gradient that reaches h by itself, NULL: none.  dx may be dy or residual.  dg [d] fp32, NULL: not computed; else
+ * workspace (16-byte aligned) of the bytes the _workspace_bytes call reports, whose contents on entry do not matter. */
+int splitlora_rmsnorm_quantize(int dtype, const void* x, const void* residual, const void* g, float eps, int64_t M, int d,
+                               void* h, void* y, int8_t* codes, int64_t ld_codes, float* scales, void* stream);
+int splitlora_rmsnorm_bwd_workspace_bytes(int64_t M, int d, size_t* bytes);
+int splitlora_rmsnorm_bwd(int dtype, const void* dy, const void* h, const void* g, const void* residual, float eps,
+                          int64_t M, int d, void* dx, float* dg, void* workspace, size_t workspace_bytes, void* stream);
+/* Linear layer over codes:  y[m,n] = (sum_k x[m,k] W[n,k]) * (x_scales[m] w_scales[n]) + bias[n] + residual[m,n]
+ * x [M, in] and W [out, in] int8, x_scales [M], w_scales [out] or NULL (ones) fp32; bias [out] or NULL, residual [M, out] or NULL
+ * and y [M, out] in `dtype`, contiguous.  The sum is exact in 32 bits (1 <= in <= 65536), the rest fp32, rounded once.  residual also
+ * takes the rank-r term of an adapter.  y may be residual.  Reports an expired wait to the library's status word. */
+int splitlora_linear_i8(int dtype, const int8_t* x, int64_t ld_x, const float* x_scales, const int8_t* W, int64_t ld_w,
+                        const float* w_scales, const void* bias, const void* residual, int M, int n_in, int n_out, void* y,
+                        void* stream);
+/* Loss over the vocabulary against a teacher's top logits and the labels, and its gradient.  Per row, with z = logits[m, 0..vocab),
+ * T = temperature, the entries j < k whose top_idx[m,j] lies in [0, vocab) (others are left out), q = softmax_j(top_logits[m,j] / T):
+ *   row_loss[m] = ce_weight (-log softmax(z)[label]) + kd_weight T^2 sum_j q_j (log q_j - log softmax(z / T)[top_idx_j])
+ *   loss        = sum_m row_loss[m] / n
+ *   dlogits     = (ce_weight (softmax(z) - [label]) + kd_weight T (softmax(z / T) - q)) / n
+ * labels [M] or NULL (then ce_weight must be 0); a row whose label lies outside [0, vocab) takes no part: loss and gradient 0.  n
+ * counts the rows that take part, or is `normalizer` where that is positive (a shard of a larger batch; cf.
+ * splitlora_set_loss_normalizer).  A row without a teacher entry, or whose entries are all -inf, has the label's term alone.  An
+ * index that occurs twice counts twice.  -inf logits have probability 0; a row with a NaN or +inf logit, or with none above
+ * -inf, becomes NaN.
+ * logits [M, ld] and dlogits [M, ld_grad] in `dtype` (the same buffer, with the same ld, or buffers that do not
+ * overlap); columns [vocab, ld_grad) of dlogits become zero.  top_idx int32 and top_logits fp32 [M, k], 1 <= k <= 256;
+ * 1e-3 <= T <= 1e3; row_loss [M], loss [1], n_valid [1] (scratch) on the device.  Nothing is returned to the host. */
+int splitlora_distill_loss(int dtype, const void* logits, int64_t ld, const int32_t* labels, const int32_t* top_idx,
+                           const float* top_logits, int M, int vocab, int k, float temperature, float ce_weight,
+                           float kd_weight, int64_t normalizer, void* dlogits, int64_t ld_grad, float* row_loss,
+                           float* loss, int32_t* n_valid, void* stream);
 /* out [cols, rows] = in [rows, cols]^T in `dtype` (for building Wt). */
 int splitlora_transpose(int dtype, const void* in, int rows, int cols, void* out, void* stream);
 

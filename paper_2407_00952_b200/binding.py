@@ -35,7 +35,9 @@ EXPORTS = [
     "splitlora_handoff_quantize",
     "splitlora_handoff_dequantize", "splitlora_round_compressed", "splitlora_set_client_ranks",
     "splitlora_library_status", "splitlora_set_client_cuts", "splitlora_lora_linear_bwd_parts",
-    "splitlora_lora_linear_fwd_parts",
+    "splitlora_lora_linear_fwd_parts", "splitlora_quantize_rows", "splitlora_dequantize_rows",
+    "splitlora_rmsnorm_quantize", "splitlora_rmsnorm_bwd_workspace_bytes", "splitlora_rmsnorm_bwd",
+    "splitlora_linear_i8", "splitlora_distill_loss",
 ]
 
 
@@ -464,3 +466,160 @@ def attention_bwd_static(qkv, o, lse, d_o, nseq, T, n_head, use_tensor_cores=Tru
                                            _ptr(d_o), nseq, T, n_head, d, _ptr(dqkv), _stream_ptr()),
         "attention_bwd_static")
     return dqkv
+
+
+# ---- adapters over a frozen weight held in 8 bits --------------------------------------------
+ERR_ARG, ERR_ALIGN = -1, -2
+
+
+def _arg(what: str, t: Optional[torch.Tensor], dtype, shape, codes: bool = False) -> int:
+    """Address of an operator's tensor (0 for None) once its place, type, shape and layout are what the call takes."""
+    if t is None:
+        return 0
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise SplitLoraError(ERR_ARG, f"{what}: on {t.device}, not on the current CUDA device")
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise SplitLoraError(ERR_ARG, f"{what}: {t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}")
+    if codes:       # rows of codes may lie further apart than they are wide
+        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise SplitLoraError(ERR_ARG, f"{what}: strides {t.stride()}")
+    elif not t.is_contiguous():
+        raise SplitLoraError(ERR_ARG, f"{what}: not contiguous")
+    return t.data_ptr()
+
+
+def _ld(codes: torch.Tensor) -> int:
+    return codes.stride(0) if codes.shape[0] > 1 else (codes.shape[1] + 15) // 16 * 16     # one row: any distance will do
+
+
+def _rows(what: str, x: torch.Tensor):
+    """(dtype id, M, d) of a matrix of activations."""
+    if x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32):
+        raise SplitLoraError(ERR_ARG, f"{what}: {x.dtype} of {x.dim()} dimensions, not a float32 or bfloat16 matrix")
+    return _dt(x), x.shape[0], x.shape[1]
+
+
+def empty_codes(M: int, d: int) -> torch.Tensor:
+    """int8 [M, d] whose rows start on 16-byte boundaries (what lets linear_i8 run on the tensor cores)."""
+    ld = (d + 15) // 16 * 16
+    t = torch.empty(M, ld, dtype=torch.int8, device="cuda")
+    return t if ld == d else t[:, :d]
+
+
+def quantize_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
+                  scales: Optional[torch.Tensor] = None):
+    """x [M, d] -> (codes int8 [M, d], scales fp32 [M]); col_scale fp32 [d] multiplies x first (splitlora_quantize_rows)."""
+    dt, M, d = _rows("x", x)
+    if codes is None:
+        codes = empty_codes(M, d)
+    if scales is None:
+        scales = torch.empty(M, dtype=torch.float32, device="cuda")
+    _rc(load().splitlora_quantize_rows(
+        dt, C.c_void_p(_arg("x", x, x.dtype, (M, d))), C.c_void_p(_arg("col_scale", col_scale, torch.float32, (d,))), C.c_int64(M), d,
+        C.c_void_p(_arg("codes", codes, torch.int8, (M, d), True)), C.c_int64(_ld(codes)),
+        C.c_void_p(_arg("scales", scales, torch.float32, (M,))), _stream_ptr()), "quantize_rows")
+    return codes, scales
+
+
+def dequantize_rows(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """codes [M, d] * scales [M] as `dtype` (splitlora_dequantize_rows)."""
+    M, d = codes.shape
+    if out is None:
+        out = torch.empty(M, d, dtype=dtype, device="cuda")
+    dt, _, _ = _rows("out", out)
+    _rc(load().splitlora_dequantize_rows(
+        dt, C.c_void_p(_arg("codes", codes, torch.int8, (M, d), True)), C.c_int64(_ld(codes)),
+        C.c_void_p(_arg("scales", scales, torch.float32, (M,))), C.c_int64(M), d, C.c_void_p(_arg("out", out, out.dtype, (M, d))),
+        _stream_ptr()), "dequantize_rows")
+    return out
+
+
+def rmsnorm_quantize(x: torch.Tensor, g: torch.Tensor, residual: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                     want_y: bool = False, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None,
+                     h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None):
+    """RMSNorm of x + residual as int8 codes (splitlora_rmsnorm_quantize): (codes, scales, h, y).  h is the sum (None without a
+    residual, unless a buffer is passed), y the normalised row in x's dtype (None unless want_y or a buffer is passed)."""
+    dt, M, d = _rows("x", x)
+    if codes is None:
+        codes = empty_codes(M, d)
+    if scales is None:
+        scales = torch.empty(M, dtype=torch.float32, device="cuda")
+    if h is None and residual is not None:
+        h = torch.empty_like(x)
+    if y is None and want_y:
+        y = torch.empty_like(x)
+    _rc(load().splitlora_rmsnorm_quantize(
+        dt, C.c_void_p(_arg("x", x, x.dtype, (M, d))), C.c_void_p(_arg("residual", residual, x.dtype, (M, d))),
+        C.c_void_p(_arg("g", g, x.dtype, (d,))), C.c_float(eps), C.c_int64(M), d, C.c_void_p(_arg("h", h, x.dtype, (M, d))),
+        C.c_void_p(_arg("y", y, x.dtype, (M, d))), C.c_void_p(_arg("codes", codes, torch.int8, (M, d), True)), C.c_int64(_ld(codes)),
+        C.c_void_p(_arg("scales", scales, torch.float32, (M,))), _stream_ptr()), "rmsnorm_quantize")
+    return codes, scales, h, y
+
+
+def rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, g: torch.Tensor, resid: Optional[torch.Tensor] = None, eps: float = 1e-5,
+                want_dg: bool = False, dx: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """Gradient of rmsnorm_quantize with respect to x (= residual) and, where want_dg, to g in fp32: (dx, dg or None)
+    (splitlora_rmsnorm_bwd); resid: the gradient that reaches h by itself."""
+    dt, M, d = _rows("h", h)
+    if dx is None:
+        dx = torch.empty_like(h)
+    dg, ws_bytes = None, 0
+    if want_dg:
+        dg = torch.empty(d, dtype=torch.float32, device="cuda")
+        if workspace is None:
+            n = C.c_size_t(0)
+            _rc(load().splitlora_rmsnorm_bwd_workspace_bytes(C.c_int64(M), d, C.byref(n)), "rmsnorm_bwd_workspace_bytes")
+            workspace = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+        ws_bytes = workspace.numel() * workspace.element_size()
+    _rc(load().splitlora_rmsnorm_bwd(
+        dt, C.c_void_p(_arg("dy", dy, h.dtype, (M, d))), C.c_void_p(_arg("h", h, h.dtype, (M, d))), C.c_void_p(_arg("g", g, h.dtype, (d,))),
+        C.c_void_p(_arg("resid", resid, h.dtype, (M, d))), C.c_float(eps), C.c_int64(M), d, C.c_void_p(_arg("dx", dx, h.dtype, (M, d))),
+        C.c_void_p(0 if dg is None else dg.data_ptr()),
+        C.c_void_p(0 if dg is None else _arg("workspace", workspace, workspace.dtype, workspace.shape)), C.c_size_t(ws_bytes),
+        _stream_ptr()), "rmsnorm_bwd")
+    return dx, dg
+
+
+def linear_i8(x: torch.Tensor, x_scales: torch.Tensor, W: torch.Tensor, w_scales: Optional[torch.Tensor] = None,
+              bias: Optional[torch.Tensor] = None, residual: Optional[torch.Tensor] = None, dtype=torch.bfloat16,
+              y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """y [M, out] = (x W^T) * x_scales[m] * w_scales[n] + bias + residual from int8 codes x [M, in], W [out, in]
+    (splitlora_linear_i8)."""
+    if x.dim() != 2 or W.dim() != 2:
+        raise SplitLoraError(ERR_ARG, "x and W are matrices of codes")
+    M, K = x.shape
+    N = W.shape[0]
+    if y is None:
+        y = torch.empty(M, N, dtype=dtype, device="cuda")
+    dt, _, _ = _rows("y", y)
+    _rc(load().splitlora_linear_i8(
+        dt, C.c_void_p(_arg("x", x, torch.int8, (M, K), True)), C.c_int64(_ld(x)), C.c_void_p(_arg("x_scales", x_scales, torch.float32, (M,))),
+        C.c_void_p(_arg("W", W, torch.int8, (N, K), True)), C.c_int64(_ld(W)),
+        C.c_void_p(_arg("w_scales", w_scales, torch.float32, (N,))), C.c_void_p(_arg("bias", bias, y.dtype, (N,))),
+        C.c_void_p(_arg("residual", residual, y.dtype, (M, N))), M, K, N, C.c_void_p(_arg("y", y, y.dtype, (M, N))), _stream_ptr()),
+        "linear_i8")
+    return y
+
+
+def distill_loss(logits: torch.Tensor, top_idx: torch.Tensor, top_logits: torch.Tensor, labels: Optional[torch.Tensor] = None,
+                 temperature: float = 1.0, ce_weight: float = 0.0, kd_weight: float = 1.0, normalizer: int = 0,
+                 vocab: Optional[int] = None, dlogits: Optional[torch.Tensor] = None):
+    """Loss against a teacher's top logits (top_idx int32, top_logits fp32 [M, k]) and labels int32 [M], with its gradient:
+    (loss, a scalar on the device, row_loss [M], dlogits like logits) (splitlora_distill_loss).  vocab: columns of logits [M, ld] in use
+    (default: all); dlogits may be logits."""
+    dt, M, ld = _rows("logits", logits)
+    if top_idx.dim() != 2:
+        raise SplitLoraError(ERR_ARG, "top_idx is a matrix [M, k]")
+    k = top_idx.shape[1]
+    if dlogits is None:
+        dlogits = torch.empty_like(logits)
+    out = torch.empty(M + 2, dtype=torch.float32, device="cuda")       # row losses, loss, count
+    p = out.data_ptr()
+    _rc(load().splitlora_distill_loss(
+        dt, C.c_void_p(_arg("logits", logits, logits.dtype, (M, ld))), C.c_int64(ld),
+        C.c_void_p(_arg("labels", labels, torch.int32, (M,))), C.c_void_p(_arg("top_idx", top_idx, torch.int32, (M, k))),
+        C.c_void_p(_arg("top_logits", top_logits, torch.float32, (M, k))), M, ld if vocab is None else int(vocab), k, C.c_float(temperature),
+        C.c_float(ce_weight), C.c_float(kd_weight), C.c_int64(normalizer),
+        C.c_void_p(_arg("dlogits", dlogits, logits.dtype, (M, ld))), C.c_int64(ld), C.c_void_p(p), C.c_void_p(p + 4 * M), C.c_void_p(p + 4 * M + 4),
+        _stream_ptr()), "distill_loss")
+    return out[M], out[:M], dlogits

@@ -1,0 +1,662 @@
+// Products of int8 codes for layers whose frozen weight is held in 8 bits:
+//   y[m, n] = round( (sum_k xq[m, k] wq[n, k]) * (sx[m] sw[n]) + bias[n] + r[m, n] )
+// The sum is exact: int8 products into 32-bit integers (K <= 65536 leaves a factor of two), so no kernel, split or order changes
+// it; the scaling, bias and residual are fp32, rounded once to the output's type.
+//   gemm_i8_pair_kernel   CTA pairs (cluster of 2, tcgen05 cta_group::2, kind::i8): tiles of 256 x 256 or 256 x 128, persistent,
+//                         accumulator double buffered in tensor memory.  A 128-deep block of codes is 128 bytes per row, the
+//                         128-byte swizzle row, and four products of depth 32; copies, ring and barriers are those of the bf16
+//                         linear layers (gemm_tc.cu), at twice the operations per byte.
+//   gemm_i8_split_kernel  few tiles: one 128 x 64 tile per cluster of 1-8 CTAs that share the contraction and add their integer
+//                         sums through distributed shared memory.
+//   gemm_i8_simt_kernel   codes whose rows do not start on 16-byte boundaries (copies cannot take them).
+// Every wait on an mbarrier is bounded; when it expires the kernel records a code in `status` and returns.
+#include "host_common.h"
+#include "launch.cuh"
+#include "tc_common.cuh"
+
+namespace sl {
+namespace {
+
+using namespace tc;
+
+constexpr int NUM_THREADS = 320;
+constexpr int KB = 128;                    // codes per block of the contraction: one swizzle row
+constexpr int TILE_BYTES = BM * KB;        // 128 rows
+
+struct I8Params {
+  int M, N, num_kb;
+  int tiles_m, tiles_n;
+  const float* sx; const float* sw;        // sw, bias, R may be null
+  const void* bias; const void* R; void* Y;
+  int* status;
+};
+
+// kind::i8 instruction descriptor: 32-bit integer accumulator, signed x signed, both operands K-major, no saturation
+__host__ __device__ constexpr uint32_t make_idesc_i8(int m, int n) {
+  return (2u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+template <int CG> __device__ __forceinline__ void mma_i8(uint32_t d_tmem, uint32_t alo, uint32_t blo, uint32_t idesc, uint32_t accumulate) {
+  if constexpr (CG == 1)
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::1.kind::i8 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(alo), "r"(blo), "r"(DESC_HI), "r"(idesc), "r"(accumulate) : "memory");
+  else
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t.reg .b64 da, db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 da, {%1, %3};\n\tmov.b64 db, {%2, %3};\n\t"
+        "tcgen05.mma.cta_group::2.kind::i8 [%0], da, db, %4, p;\n\t}"
+        ::"r"(d_tmem), "r"(alo), "r"(blo), "r"(DESC_HI), "r"(idesc), "r"(accumulate) : "memory");
+}
+// the four products of one block; advancing 32 codes along K inside the swizzled row is +2 in descriptor units
+template <int CG> __device__ __forceinline__ void mma_block(uint32_t d_tmem, uint32_t alo, uint32_t blo, uint32_t idesc, bool first) {
+  mma_i8<CG>(d_tmem, alo, blo, idesc, first ? 0u : 1u);
+  mma_i8<CG>(d_tmem, alo + 2, blo + 2, idesc, 1u);
+  mma_i8<CG>(d_tmem, alo + 4, blo + 4, idesc, 1u);
+  mma_i8<CG>(d_tmem, alo + 6, blo + 6, idesc, 1u);
+}
+
+__device__ __forceinline__ void lds4(float* v, uint32_t addr) {
+  asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[0]), "=f"(v[1]), "=f"(v[2]), "=f"(v[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void sts1(uint32_t addr, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory"); }
+__device__ __forceinline__ float lds1(uint32_t addr) {
+  float v;
+  asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
+  return v;
+}
+
+// Channel scale and bias of column n + lane (1 and 0 where there is none, 0 past the last column).
+template <typename TO> __device__ __forceinline__ void load_channel(const I8Params& p, int n, int lane, float& sw, float& b) {
+  const int c = n + lane;
+  sw = c < p.N ? (p.sw ? __ldg(p.sw + c) : 1.0f) : 0.f;
+  b = c < p.N && p.bias ? to_f<TO>(reinterpret_cast<const TO*>(p.bias)[c]) : 0.f;
+}
+
+// One 32-row x 32-column chunk of accumulators (acc: this thread's row, columns [n, n + 32)) to the output.  `stage`: 4 KB of this
+// warp.  Channel scales and biases arrive one per lane and go round through shared memory, which any N and type allow.
+// VEC: output (and residual) rows on 16-byte boundaries, bf16: staged like the bf16 layers' and stored by TMA.  Else each row of
+// the chunk leaves as one coalesced store of a warp.
+template <typename TO, bool VEC>
+__device__ __forceinline__ void i8_chunk(const I8Params& p, const uint32_t* acc, float sx, float sw_lane, float b_lane, int m_warp0, int n, int lane,
+                                         uint32_t stage, int& buf, const CUtensorMap* mapY) {
+  const uint32_t sbuf = VEC ? stage + (uint32_t)buf * 2048u : stage;
+  uint4 r[4];
+  if constexpr (VEC) {
+    if (p.R) {
+      const bf16* rrow = reinterpret_cast<const bf16*>(p.R) + (size_t)(m_warp0 + lane) * p.N + n;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        r[j] = n + 8 * j < p.N && m_warp0 + lane < p.M ? __ldg(reinterpret_cast<const uint4*>(rrow + 8 * j)) : make_uint4(0u, 0u, 0u, 0u);
+    }
+    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");     // the store that last read this buffer
+  }
+  __syncwarp();
+  sts1(sbuf + 4u * lane, sw_lane);
+  sts1(sbuf + 128u + 4u * lane, b_lane);
+  __syncwarp();
+  float v[32];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float w[4], b[4];
+    lds4(w, sbuf + 16u * j);
+    lds4(b, sbuf + 128u + 16u * j);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[4 * j + i] = fmaf(__int2float_rn((int)acc[4 * j + i]), sx * w[i], b[i]);
+  }
+  __syncwarp();
+  if constexpr (VEC) {
+    if (p.R) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t w[4] = {r[j].x, r[j].y, r[j].z, r[j].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { v[8 * j + 2 * i] += __uint_as_float(w[i] << 16); v[8 * j + 2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u); }
+      }
+    }
+    uint32_t packed[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      __nv_bfloat162 y2 = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      packed[i] = *reinterpret_cast<uint32_t*>(&y2);
+    }
+    stage_and_store(sbuf, mapY, packed, lane, n, m_warp0);       // clipped at row M and column N
+    buf ^= 1;
+  } else {
+    // word (row, column) at column ^ row of its row: no two lanes of a store or a load share a bank
+#pragma unroll
+    for (int i = 0; i < 32; ++i) sts1(sbuf + (uint32_t)lane * 128u + (uint32_t)((i ^ lane) << 2), v[i]);
+    __syncwarp();
+    const int rows = min(32, p.M - m_warp0);
+    TO* y = reinterpret_cast<TO*>(p.Y);
+    const TO* res = reinterpret_cast<const TO*>(p.R);
+    if (n + lane < p.N) {
+#pragma unroll 4
+      for (int q = 0; q < rows; ++q) {
+        const size_t at = (size_t)(m_warp0 + q) * p.N + n + lane;
+        float t = lds1(sbuf + (uint32_t)q * 128u + (uint32_t)((lane ^ q) << 2));
+        if (res) t += to_f<TO>(res[at]);
+        y[at] = from_f<TO>(t);
+      }
+    }
+    __syncwarp();
+  }
+}
+
+// A warp's columns [c_begin, c_end) of the 32 rows from m_warp0 of a tile whose accumulator row is at t_row.
+template <typename TO, bool VEC>
+__device__ __forceinline__ void i8_tile(const I8Params& p, uint32_t t_row, float sx, int m_warp0, int n0, int c_begin, int c_end, int lane, uint32_t stage,
+                                        int& buf, const CUtensorMap* mapY, float sw, float b) {
+#pragma unroll 1
+  for (int c = c_begin; c < c_end; c += 32) {
+    const int n = n0 + c;
+    if (n >= p.N) break;
+    float sw_next = 0.f, b_next = 0.f;
+    if (c + 32 < c_end) load_channel<TO>(p, n + 32, lane, sw_next, b_next);
+    uint32_t acc[32];
+    tc_ld32(t_row + (uint32_t)c, reinterpret_cast<float*>(acc));
+    tc_wait_ld();
+    i8_chunk<TO, VEC>(p, acc, sx, sw, b, m_warp0, n, lane, stage, buf, mapY);
+    sw = sw_next; b = b_next;
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// CTA pairs
+// ------------------------------------------------------------------------------------------
+template <int BN_> struct PairCfg {
+  static constexpr int BN = BN_;
+  static constexpr int A_BYTES = TILE_BYTES;             // this CTA's 128 rows of x
+  static constexpr int B_BYTES = (BN / 2) * KB;          // this CTA's half of the weight tile
+  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int STAGES = BN == 256 ? 6 : 8;
+  static constexpr int TMEM_COLS = 2 * BN;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_STAGE_BYTES + 1024 + 256;
+  static constexpr uint32_t IDESC = make_idesc_i8(2 * BM, BN);
+};
+
+template <typename TO, bool VEC, int BN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
+gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapY,
+                    I8Params p) {
+  using C = PairCfg<BN>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - raw);
+  const uint32_t epi_base = base + C::STAGES * C::STAGE_BYTES;
+  const uint32_t bar_base = epi_base + EPI_STAGE_BYTES;
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };                         // used in the leader
+  auto empty_bar = [&](int s) { return bar_base + 8u * (C::STAGES + s); };          // one per CTA
+  auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * C::STAGES + a); };      // one per CTA
+  auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * C::STAGES + 2 + a); }; // used in the leader
+  uint8_t* tail = base_ptr + C::STAGES * C::STAGE_BYTES + EPI_STAGE_BYTES + 8 * (2 * C::STAGES + 4);
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t rank = cluster_ctarank();           // 0 = leader of the pair
+  const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 16); }
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32((const void*)tmem_slot)), "r"((uint32_t)C::TMEM_COLS) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();                                // the partner's barriers are initialised too
+  tc_fence_after();
+  const uint32_t tmem_base = *tmem_slot;
+  overlap_sync();
+
+  const int num_tiles = p.tiles_m * p.tiles_n;       // tiles of 256 x BN
+
+  if (warp == 0) {
+    // ---------------- TMA producer (both CTAs) ----------------
+    const bool leader = elect_one();
+    int stage = 0; uint32_t phase = 0;
+    bool ok = true;
+    for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
+      int tm, tn; tile_coords(tile, p.tiles_m, p.tiles_n, tm, tn);
+      const int m0 = tm * 2 * BM + (int)rank * BM, n0 = tn * BN + (int)rank * (BN / 2);
+      for (int kb = 0; kb < p.num_kb; ++kb) {
+        if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, p.status, 61)) { ok = false; break; }
+        const uint32_t leader_full = map_to_cta(full_bar(stage), 0);
+        const uint32_t sa = base + stage * C::STAGE_BYTES, sb = sa + C::A_BYTES;
+        if (leader) {
+          // the first CTA's barrier collects the bytes of both CTAs' copies
+          if (rank == 0) mbar_expect_tx(full_bar(stage), 2 * C::STAGE_BYTES);
+          tma_load_2d_pair(sa, &mapX, leader_full, kb * KB, m0);
+          tma_load_2d_pair(sb, &mapW, leader_full, kb * KB, n0);
+        }
+        __syncwarp();
+        if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------- MMA issuer (first CTA of the pair only) ----------------
+    if (rank == 0) {
+      const bool leader = elect_one();
+      int stage = 0; uint32_t phase = 0;
+      int as = 0; uint32_t aphase = 0;
+      bool ok = true;
+      const uint32_t a_lo0 = desc_lo(base);
+      for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
+        if (!mbar_wait_warp(tempty_bar(as), aphase ^ 1u, abort_flag, p.status, 62)) { ok = false; break; }
+        tc_fence_after();
+        const uint32_t d_tmem = tmem_base + (uint32_t)(as * BN);
+        for (int kb = 0; kb < p.num_kb; ++kb) {
+          if (!mbar_wait_warp(full_bar(stage), phase, abort_flag, p.status, 63)) { ok = false; break; }
+          const uint32_t alo = a_lo0 + (uint32_t)stage * (uint32_t)(C::STAGE_BYTES >> 4);
+          const uint32_t blo = alo + (uint32_t)(C::A_BYTES >> 4);
+          if (leader) {
+            mma_block<2>(d_tmem, alo, blo, C::IDESC, kb == 0);
+            tc_commit_pair(empty_bar(stage), 3);     // frees the stage in both CTAs
+          }
+          __syncwarp();
+          if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+        }
+        if (!ok) break;
+        if (leader) tc_commit_pair(tfull_bar(as), 3);
+        __syncwarp();
+        if (++as == 2) { as = 0; aphase ^= 1u; }
+      }
+    }
+  } else {
+    // ---------------- epilogue (both CTAs, own 128 rows) ----------------
+    const int q = warp & 3;
+    const int half = (warp - 2) >> 2;
+    const int c_begin = half * (BN / 2), c_end = c_begin + BN / 2;
+    int as = 0; uint32_t aphase = 0;
+    const uint32_t stage = epi_base + (uint32_t)(warp - 2) * 4096u;
+    int buf = 0;
+    bool ok = true;
+    for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
+      int tm, tn; tile_coords(tile, p.tiles_m, p.tiles_n, tm, tn);
+      const int m_warp0 = tm * 2 * BM + (int)rank * BM + q * 32;
+      const int n0 = tn * BN;
+      // in flight while the accumulator is awaited
+      const float sx = m_warp0 + lane < p.M ? __ldg(p.sx + m_warp0 + lane) : 0.f;
+      float sw, b;
+      load_channel<TO>(p, n0 + c_begin, lane, sw, b);
+      if (!mbar_wait(tfull_bar(as), aphase, abort_flag, p.status, 64)) { ok = false; break; }
+      tc_fence_after();
+      const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(as * BN);
+      if (m_warp0 < p.M) i8_tile<TO, VEC>(p, t_row, sx, m_warp0, n0, c_begin, c_end, lane, stage, buf, &mapY, sw, b);
+      tc_fence_before();
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(as), 0));   // 16 arrivals free the stage
+      if (++as == 2) { as = 0; aphase ^= 1u; }
+    }
+    epilogue_drain(lane);
+  }
+
+  // ---------------- teardown ----------------
+  __syncwarp();
+  if (*abort_flag) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  }
+  tc_fence_before();
+  __syncthreads();
+  cluster_sync_all();                                // neither CTA leaves while its partner may still touch it
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::TMEM_COLS) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// few tiles: one 128 x 64 tile per cluster, the contraction split over its S CTAs
+// ------------------------------------------------------------------------------------------
+// Every CTA contracts its range of blocks into its own tensor memory; piece (warp) u of the tile, 32 x 32 accumulators, is added
+// up by CTA u % S from what the others sent it through distributed shared memory.
+template <int S> struct SplitCfg {
+  static constexpr int BN = 64;
+  static constexpr int A_BYTES = TILE_BYTES;
+  static constexpr int B_BYTES = BN * KB;
+  static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
+  static constexpr int STAGES = 7;
+  static constexpr int RECV_BYTES = (8 / S) * (S - 1) * 4096;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + RECV_BYTES + 1024 + 256;
+  static constexpr uint32_t IDESC = make_idesc_i8(BM, BN);
+  static_assert(STAGES * STAGE_BYTES >= EPI_STAGE_BYTES && 8 % S == 0 && SMEM_BYTES <= 232448, "");
+};
+
+template <typename TO, bool VEC, int S>
+__global__ void __launch_bounds__(NUM_THREADS, 1)
+gemm_i8_split_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapY,
+                     I8Params p) {
+  using C = SplitCfg<S>;
+  extern __shared__ uint8_t smem_raw[];
+  const uint32_t raw = smem_u32(smem_raw);
+  const uint32_t base = (raw + 1023u) & ~1023u;
+  uint8_t* base_ptr = smem_raw + (base - raw);
+  const uint32_t recv_base = base + C::STAGES * C::STAGE_BYTES;
+  const uint32_t bar_base = recv_base + C::RECV_BYTES;
+  auto full_bar = [&](int s) { return bar_base + 8u * s; };
+  auto empty_bar = [&](int s) { return bar_base + 8u * (C::STAGES + s); };
+  const uint32_t tfull_bar = bar_base + 8u * (2 * C::STAGES);
+  uint8_t* tail = base_ptr + C::STAGES * C::STAGE_BYTES + C::RECV_BYTES + 8 * (2 * C::STAGES + 1);
+  volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
+  volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8);
+
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = S > 1 ? (int)cluster_ctarank() : 0;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
+    mbar_init(tfull_bar, 1);
+    *abort_flag = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;"
+                 ::"r"(smem_u32((const void*)tmem_slot)), "r"((uint32_t)C::BN) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  if (S > 1) cluster_arrive();                       // awaited before the first store to another CTA
+  const uint32_t tmem_base = *tmem_slot;
+  overlap_sync();
+
+  const int kb0 = (int)((long long)p.num_kb * rank / S), kb1 = (int)((long long)p.num_kb * (rank + 1) / S);   // never empty: num_kb >= S
+  int tm, tn;
+  tile_coords((int)blockIdx.x / S, p.tiles_m, p.tiles_n, tm, tn);
+  const int m0 = tm * BM, n0 = tn * C::BN;
+
+  if (warp == 0) {
+    const bool leader = elect_one();
+    int stage = 0; uint32_t phase = 0;
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, p.status, 71)) break;
+      const uint32_t sa = base + stage * C::STAGE_BYTES, sb = sa + C::A_BYTES;
+      if (leader) {
+        mbar_expect_tx(full_bar(stage), C::STAGE_BYTES);
+        tma_load_2d(sb, &mapW, full_bar(stage), kb * KB, n0);
+        tma_load_2d(sa, &mapX, full_bar(stage), kb * KB, m0);
+      }
+      __syncwarp();
+      if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+    }
+  } else if (warp == 1) {
+    const bool leader = elect_one();
+    int stage = 0; uint32_t phase = 0;
+    bool ok = true;
+    const uint32_t a_lo0 = desc_lo(base);
+    for (int kb = kb0; kb < kb1; ++kb) {
+      if (!mbar_wait_warp(full_bar(stage), phase, abort_flag, p.status, 73)) { ok = false; break; }
+      const uint32_t alo = a_lo0 + (uint32_t)stage * (uint32_t)(C::STAGE_BYTES >> 4);
+      if (leader) {
+        mma_block<1>(tmem_base, alo, alo + (uint32_t)(C::A_BYTES >> 4), C::IDESC, kb == kb0);
+        tc_commit(empty_bar(stage));
+      }
+      __syncwarp();
+      if (++stage == C::STAGES) { stage = 0; phase ^= 1u; }
+    }
+    if (ok && leader) tc_commit(tfull_bar);
+  }
+  __syncwarp();
+
+  // ---------------- epilogue ----------------
+  const int ew = warp - 2;                           // epilogue warp 0..7
+  const int q = warp & 3, half = ew >> 2;
+  const int m_warp0 = m0 + q * 32, n = n0 + 32 * half;
+  const int u = half * 4 + q, owner = u % S;         // this warp's piece and the CTA that adds it up
+  const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(32 * half);
+  const bool live = warp >= 2 && m_warp0 < p.M && n < p.N;
+  uint32_t acc[32];
+  float sx = 0.f, sw = 0.f, b = 0.f;
+  bool ok = false;
+  if (warp >= 2) {
+    if (live && owner == rank) {
+      sx = m_warp0 + lane < p.M ? __ldg(p.sx + m_warp0 + lane) : 0.f;
+      load_channel<TO>(p, n, lane, sw, b);
+    }
+    ok = mbar_wait(tfull_bar, 0u, abort_flag, p.status, 74);
+    tc_fence_after();
+    if (live && ok) {
+      tc_ld32(t_row, reinterpret_cast<float*>(acc));
+      tc_wait_ld();
+    }
+  }
+  if constexpr (S > 1) {
+    __syncwarp();
+    cluster_wait();                                  // every CTA of the cluster runs: its shared memory exists
+    if (live && ok && owner != rank) {
+      const int sender = rank < owner ? rank : rank - 1;
+      const uint32_t dst = map_to_cta(recv_base + (uint32_t)(((u / S) * (S - 1) + sender) * 4096 + lane * 16), (uint32_t)owner);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(dst + (uint32_t)(i * 512)), "r"(acc[4 * i]), "r"(acc[4 * i + 1]),
+                     "r"(acc[4 * i + 2]), "r"(acc[4 * i + 3]) : "memory");
+    }
+    __syncwarp();
+    cluster_sync_all();
+  }
+  if (live && ok && owner == rank) {
+    if constexpr (S > 1) {
+#pragma unroll
+      for (int s = 0; s < S - 1; ++s) {
+        const uint32_t src = recv_base + (uint32_t)(((u / S) * (S - 1) + s) * 4096 + lane * 16);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint32_t x0, x1, x2, x3;
+          asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(x0), "=r"(x1), "=r"(x2), "=r"(x3) : "r"(src + (uint32_t)(i * 512)) : "memory");
+          acc[4 * i] += x0; acc[4 * i + 1] += x1; acc[4 * i + 2] += x2; acc[4 * i + 3] += x3;
+        }
+      }
+    }
+    int buf = 0;
+    // the output staging takes the operand ring, which is idle: every product has completed
+    i8_chunk<TO, VEC>(p, acc, sx, sw, b, m_warp0, n, lane, base + (uint32_t)ew * 4096u, buf, &mapY);
+  }
+  if (warp >= 2) epilogue_drain(lane);
+
+  __syncwarp();
+  if (*abort_flag) {
+    for (int i = 0; i < 2000; ++i) __nanosleep(1000);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == 1) {
+    tc_fence_after();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::BN) : "memory");
+  }
+}
+
+// ------------------------------------------------------------------------------------------
+// any alignment: 64 x 64 tiles, four codes per instruction (dp4a) from shared memory
+// ------------------------------------------------------------------------------------------
+template <typename TO>
+__global__ void __launch_bounds__(256)
+gemm_i8_simt_kernel(const int8_t* __restrict__ x, int64_t ldx, const int8_t* __restrict__ w, int64_t ldw, int K, I8Params p) {   // tiles_m x tiles_n blocks
+  overlap_sync();
+  constexpr int T = 64, D = 64;
+  __shared__ __align__(16) int8_t xs[T][D + 4], ws[T][D + 4];
+  const int m0 = (int)(blockIdx.x / p.tiles_n) * T, n0 = (int)(blockIdx.x % p.tiles_n) * T;
+  const int tm = threadIdx.x >> 4, tn = threadIdx.x & 15;      // rows tm + 16 i, columns tn + 16 j
+  int acc[4][4] = {};
+  for (int k0 = 0; k0 < K; k0 += D) {
+    for (int e = threadIdx.x; e < T * D; e += 256) {
+      const int r = e / D, c = e % D;
+      xs[r][c] = m0 + r < p.M && k0 + c < K ? x[(int64_t)(m0 + r) * ldx + k0 + c] : (int8_t)0;
+      ws[r][c] = n0 + r < p.N && k0 + c < K ? w[(int64_t)(n0 + r) * ldw + k0 + c] : (int8_t)0;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int c = 0; c < D; c += 4) {
+      int a[4], b[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        a[i] = *reinterpret_cast<const int*>(&xs[tm + 16 * i][c]);
+        b[i] = *reinterpret_cast<const int*>(&ws[tn + 16 * i][c]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = __dp4a(a[i], b[j], acc[i][j]);
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int m = m0 + tm + 16 * i;
+    if (m >= p.M) continue;
+    const float sx = p.sx[m];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int n = n0 + tn + 16 * j;
+      if (n >= p.N) continue;
+      const size_t at = (size_t)m * p.N + n;
+      float v = fmaf(__int2float_rn(acc[i][j]), sx * (p.sw ? p.sw[n] : 1.0f), p.bias ? to_f<TO>(reinterpret_cast<const TO*>(p.bias)[n]) : 0.f);
+      if (p.R) v += to_f<TO>(reinterpret_cast<const TO*>(p.R)[at]);
+      reinterpret_cast<TO*>(p.Y)[at] = from_f<TO>(v);
+    }
+  }
+}
+
+// ---- host side -----------------------------------------------------------------------------
+int g_pairs[MAX_DEVICES] = {};                   // CTA pairs that can be resident at once
+int g_clusters[MAX_DEVICES][3] = {};             // clusters of 2, 4 and 8 CTAs
+PerDeviceOnce g_once;
+
+bool map_codes(CUtensorMap* m, const void* ptr, int64_t rows, int64_t cols, int64_t ld, uint32_t box_rows) {
+  return cached_map_2d_u8(m, ptr, rows, cols, ld, KB, box_rows, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
+}
+
+template <typename K> int clusters_resident(K kernel, int size, int smem) {
+  if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(size); cfg.blockDim = dim3(NUM_THREADS); cfg.dynamicSmemBytes = smem;
+  cudaLaunchAttribute at;
+  at.id = cudaLaunchAttributeClusterDimension;
+  at.val.clusterDim.x = size; at.val.clusterDim.y = 1; at.val.clusterDim.z = 1;
+  cfg.attrs = &at; cfg.numAttrs = 1;
+  int n = 0;
+  return cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) == cudaSuccess ? n : 0;
+}
+
+template <typename K> cudaError_t allow_smem(K kernel, PerDeviceOnce& once, int smem) {
+  const int dev = current_device();
+  if (!once.needed(dev)) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  if (e == cudaSuccess) once.done(dev);
+  return e;
+}
+
+template <typename TO, bool VEC, int BN> cudaError_t launch_pair(const I8Args& a, I8Params p, CUtensorMap mX, CUtensorMap mY, cudaStream_t st) {
+  using C = PairCfg<BN>;
+  static PerDeviceOnce once;
+  const cudaError_t e = allow_smem(gemm_i8_pair_kernel<TO, VEC, BN>, once, C::SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  CUtensorMap mW;
+  if (!map_codes(&mW, a.W, a.N, a.K, a.ldw, BN / 2)) return cudaErrorInvalidValue;
+  p.tiles_m = (a.M + 2 * BM - 1) / (2 * BM); p.tiles_n = (a.N + BN - 1) / BN;
+  const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
+  const int most = g_pairs[current_device()], pairs = tiles < most ? (int)tiles : most;
+  return launch_overlapped(gemm_i8_pair_kernel<TO, VEC, BN>, dim3(2 * pairs), dim3(NUM_THREADS), C::SMEM_BYTES, st, mX, mW, mY, p);
+}
+
+template <typename TO, bool VEC, int S> cudaError_t launch_split(const I8Args& a, I8Params p, CUtensorMap mX, CUtensorMap mY, cudaStream_t st) {
+  using C = SplitCfg<S>;
+  static PerDeviceOnce once;
+  const cudaError_t e = allow_smem(gemm_i8_split_kernel<TO, VEC, S>, once, C::SMEM_BYTES);
+  if (e != cudaSuccess) return e;
+  CUtensorMap mW;
+  if (!map_codes(&mW, a.W, a.N, a.K, a.ldw, C::BN)) return cudaErrorInvalidValue;
+  p.tiles_m = (a.M + BM - 1) / BM; p.tiles_n = (a.N + C::BN - 1) / C::BN;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3((unsigned)(p.tiles_m * p.tiles_n * S)); cfg.blockDim = dim3(NUM_THREADS);
+  cfg.dynamicSmemBytes = C::SMEM_BYTES; cfg.stream = st;
+  cudaLaunchAttribute at[2];
+  at[0].id = cudaLaunchAttributeClusterDimension;
+  at[0].val.clusterDim.x = S; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
+  cfg.attrs = at; cfg.numAttrs = chain_attribute(at, 1);
+  return cudaLaunchKernelEx(&cfg, gemm_i8_split_kernel<TO, VEC, S>, mX, mW, mY, p);
+}
+
+// The kernel with the least estimated time (ns): a fixed part, the time of a 128-deep block, rounds over the chip.
+enum Pick { PICK_PAIR256, PICK_PAIR128, PICK_SPLIT1, PICK_SPLIT2, PICK_SPLIT4, PICK_SPLIT8 };
+Pick pick(const I8Args& a) {
+  const int dev = current_device();
+  const int64_t sms = num_sms(), kb = (a.K + KB - 1) / KB;
+  auto cdiv = [](int64_t x, int64_t y) { return (x + y - 1) / y; };
+  Pick best = PICK_SPLIT1;
+  int64_t best_ns = INT64_MAX;
+  auto offer = [&](Pick k, int64_t ns) { if (ns < best_ns) { best_ns = ns; best = k; } };
+  auto split = [&](Pick k, int s, int64_t slots, int64_t fixed) {
+    if (slots < 1 || kb < 2 * s) { if (s > 1) return; }
+    const int64_t rounds = cdiv(cdiv(a.M, BM) * cdiv(a.N, 64), slots < 1 ? sms : slots);
+    offer(k, fixed + rounds * cdiv(kb, s) * 190 + (rounds - 1) * 3000);
+  };
+  split(PICK_SPLIT1, 1, sms, 3600);
+  split(PICK_SPLIT2, 2, g_clusters[dev][0], 4700);
+  split(PICK_SPLIT4, 4, g_clusters[dev][1], 5000);
+  split(PICK_SPLIT8, 8, g_clusters[dev][2], 5500);
+  if (g_pairs[dev] > 0 && a.M > BM) {
+    offer(PICK_PAIR256, 5500 + cdiv(cdiv(a.M, 2 * BM) * cdiv(a.N, 256), g_pairs[dev]) * kb * 275);
+    offer(PICK_PAIR128, 4500 + cdiv(cdiv(a.M, 2 * BM) * cdiv(a.N, 128), g_pairs[dev]) * kb * 200);
+  }
+  return best;
+}
+
+template <typename TO, bool VEC> cudaError_t launch_tc(const I8Args& a, const I8Params& p, cudaStream_t st) {
+  CUtensorMap mX, mY;
+  if (!map_codes(&mX, a.X, a.M, a.K, a.ldx, BM)) return cudaErrorInvalidValue;
+  mY = mX;
+  if (VEC && !cached_map_2d(&mY, a.Y, a.M, a.N, a.N, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE)) return cudaErrorInvalidValue;
+  switch (pick(a)) {
+    case PICK_PAIR256: return launch_pair<TO, VEC, 256>(a, p, mX, mY, st);
+    case PICK_PAIR128: return launch_pair<TO, VEC, 128>(a, p, mX, mY, st);
+    case PICK_SPLIT2: return launch_split<TO, VEC, 2>(a, p, mX, mY, st);
+    case PICK_SPLIT4: return launch_split<TO, VEC, 4>(a, p, mX, mY, st);
+    case PICK_SPLIT8: return launch_split<TO, VEC, 8>(a, p, mX, mY, st);
+    default: return launch_split<TO, VEC, 1>(a, p, mX, mY, st);
+  }
+}
+
+bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+}  // namespace
+
+int gemm_i8_init() {
+  if (!tensor_map_encoder()) return -1;
+  const int dev = current_device(), sms = num_sms();
+  if (dev < 0 || sms < 1) return -1;
+  if (!g_once.needed(dev)) return 0;
+  const int pairs = clusters_resident(gemm_i8_pair_kernel<bf16, true, 256>, 2, PairCfg<256>::SMEM_BYTES);
+  g_pairs[dev] = pairs < sms / 2 ? pairs : sms / 2;
+  g_clusters[dev][0] = clusters_resident(gemm_i8_split_kernel<bf16, true, 2>, 2, SplitCfg<2>::SMEM_BYTES);
+  g_clusters[dev][1] = clusters_resident(gemm_i8_split_kernel<bf16, true, 4>, 4, SplitCfg<4>::SMEM_BYTES);
+  g_clusters[dev][2] = clusters_resident(gemm_i8_split_kernel<bf16, true, 8>, 8, SplitCfg<8>::SMEM_BYTES);
+  cudaGetLastError();
+  g_once.done(dev);
+  return 0;
+}
+
+cudaError_t gemm_i8(const I8Args& a, int* status, cudaStream_t st) {
+  I8Params p = {};
+  p.M = a.M; p.N = a.N; p.num_kb = (a.K + KB - 1) / KB;
+  p.sx = a.x_scales; p.sw = a.w_scales; p.bias = a.bias; p.R = a.R; p.Y = a.Y; p.status = status;
+  if (a.ldx % 16 != 0 || a.ldw % 16 != 0 || !al16(a.X) || !al16(a.W)) {
+    p.tiles_m = (a.M + 63) / 64; p.tiles_n = (a.N + 63) / 64;
+    const dim3 grid((unsigned)p.tiles_m * (unsigned)p.tiles_n);
+    if (a.dtype == DT_BF16) return launch_overlapped(gemm_i8_simt_kernel<bf16>, grid, dim3(256), 0, st, a.X, a.ldx, a.W, a.ldw, a.K, p);
+    return launch_overlapped(gemm_i8_simt_kernel<float>, grid, dim3(256), 0, st, a.X, a.ldx, a.W, a.ldw, a.K, p);
+  }
+  if (a.dtype != DT_BF16) return launch_tc<float, false>(a, p, st);
+  if (a.N % 8 == 0 && al16(a.Y) && al16(a.R)) return launch_tc<bf16, true>(a, p, st);
+  return launch_tc<bf16, false>(a, p, st);
+}
+
+}  // namespace sl

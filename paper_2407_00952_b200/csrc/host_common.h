@@ -44,4 +44,8 @@ bool cached_map_2d(CUtensorMap* out, const void* ptr, uint64_t rows, uint64_t co
 bool cached_map_3d(CUtensorMap* out, const void* ptr, uint64_t planes, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t plane_ld,
                    uint32_t box_cols, uint32_t box_rows, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promo);
 
+// A 2-D map of bytes: cols, ld and box_cols in bytes (ld a multiple of 16); columns past `cols` are filled with zeros.
+bool cached_map_2d_u8(CUtensorMap* out, const void* ptr, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_cols,
+                      uint32_t box_rows, CUtensorMapSwizzle swizzle, CUtensorMapL2promotion promo);
+
 }  // namespace sl

@@ -239,4 +239,37 @@ cudaError_t handoff_quantize(int dt, const void* x, int64_t M, int d, uint8_t* c
 cudaError_t handoff_dequantize(int dt, const uint8_t* codes, const float* scales, int64_t M, int d, void* y,
                                cudaStream_t st);
 
+// Rows in 8 bits (quant_rows.cu): codes int8 [M, d] with rows ldc apart, one fp32 scale per row.  factor: column factors [d] or null.
+constexpr int ROWS_MAX_WIDTH = 16384;    // of a norm: a row stays in the registers of at most 1024 threads
+constexpr int QUANT_MAX_WIDTH = 65536;   // of codes: sums of that many products of codes fit 32 bits twice over
+cudaError_t quantize_rows(int dt, const void* x, const float* factor, int64_t M, int d, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st);
+cudaError_t dequantize_rows(int dt, const int8_t* codes, int64_t ldc, const float* scales, int64_t M, int d, void* y, cudaStream_t st);
+// RMSNorm of x + resid (resid, h, y may be null) with int8 output; h: the sum, y: the normalised row, in dt.
+cudaError_t rmsnorm_quantize(int dt, const void* x, const void* resid, const void* g, int64_t M, int d, float eps, void* h, void* y, int8_t* codes,
+                             int64_t ldc, float* scales, cudaStream_t st);
+// dx = resid + d/dh (resid may be null); dg (may be null) fp32 [d] with partial of at least rmsnorm_dg_scratch_floats.
+constexpr int DG_PARTIAL_ROWS = 592;
+size_t rmsnorm_dg_scratch_floats(int64_t M, int d);
+cudaError_t rmsnorm_gain_bwd(int dt, const void* dy, const void* h, const void* g, const void* resid, int64_t M, int d, float eps, void* dx, float* dg,
+                             float* partial, cudaStream_t st);
+
+// Products of int8 codes (gemm_i8.cu): Y[M, N] = (X W^T) * (x_scales[m] w_scales[n]) + bias + R; w_scales, bias and R may be null;
+// X [M, K] and W [N, K] int8 with rows ldx, ldw apart; bias, R, Y in dtype, R and Y contiguous.
+struct I8Args {
+  int dtype = DT_BF16, M = 0, N = 0, K = 0;
+  const int8_t *X = nullptr, *W = nullptr; int64_t ldx = 0, ldw = 0;
+  const float *x_scales = nullptr, *w_scales = nullptr;
+  const void *bias = nullptr, *R = nullptr; void* Y = nullptr;
+};
+int gemm_i8_init();
+cudaError_t gemm_i8(const I8Args& a, int* status, cudaStream_t st);
+
+// Loss against a teacher's top logits and labels (distill.cu).  logits [M, ld], grad [M, ldo] in dt (grad may be logits with ldo = ld;
+// columns [V, ldo) become zero), labels [M] or null, idx and t [M, k], rows fp32 [M].  normalizer > 0 replaces the number of
+// valid rows.
+constexpr int DISTILL_MAX_K = 256;
+cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* labels, const int32_t* idx, const float* t, int M, int V, int k,
+                    float temperature, float wc, float wk, int normalizer, void* grad, int64_t ldo, float* rows, int* n_valid, float* loss,
+                    cudaStream_t st);
+
 }  // namespace sl
