@@ -70,6 +70,8 @@ def load():
         _lib.splitlora_last_error.restype = C.c_char_p
         for name in EXPORTS:
             getattr(_lib, name)
+        for name, types in _ARGTYPES.items():
+            getattr(_lib, name).argtypes = types
     return _lib
 
 
@@ -469,68 +471,102 @@ def attention_bwd_static(qkv, o, lse, d_o, nseq, T, n_head, use_tensor_cores=Tru
 
 
 # ---- adapters over a frozen weight held in 8 bits --------------------------------------------
+# These calls are short enough (4-10 us on the device) for the host's share to count: argument types are declared once, so that
+# plain integers pass, and a tensor is checked in four comparisons (calls of 16-22 us -> 8-11).
 ERR_ARG, ERR_ALIGN = -1, -2
+_P, _I, _L, _F, _Z = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
+_ARGTYPES = {
+    "splitlora_quantize_rows": (_I, _P, _P, _L, _I, _P, _L, _P, _P),
+    "splitlora_dequantize_rows": (_I, _P, _L, _P, _L, _I, _P, _P),
+    "splitlora_rmsnorm_quantize": (_I, _P, _P, _P, _F, _L, _I, _P, _P, _P, _L, _P, _P),
+    "splitlora_rmsnorm_bwd_workspace_bytes": (_L, _I, _P),
+    "splitlora_rmsnorm_bwd": (_I, _P, _P, _P, _P, _F, _L, _I, _P, _P, _P, _Z, _P),
+    "splitlora_linear_i8": (_I, _P, _L, _P, _P, _L, _P, _P, _P, _I, _I, _I, _P, _P),
+    "splitlora_distill_loss": (_I, _P, _L, _P, _P, _P, _I, _I, _I, _F, _F, _F, _L, _P, _L, _P, _P, _P, _P),
+}
+_F32, _BF16, _I8, _I32 = torch.float32, torch.bfloat16, torch.int8, torch.int32
+_DTYPE_ID = {_F32: DTYPE_FP32, _BF16: DTYPE_BF16}
+_raw_stream = torch._C._cuda_getCurrentRawStream      # the current stream's handle without a Stream object (3 us)
 
 
-def _arg(what: str, t: Optional[torch.Tensor], dtype, shape, codes: bool = False) -> int:
-    """Address of an operator's tensor (0 for None) once its place, type, shape and layout are what the call takes."""
+def _refuse(what: str, t: torch.Tensor, dtype, shape, dev: int):
+    if t.get_device() != dev:
+        why = f"on {t.device}, not on the current CUDA device"
+    elif t.dtype != dtype or t.shape != shape:
+        why = f"{t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}"
+    else:
+        why = f"strides {t.stride()}"
+    raise SplitLoraError(ERR_ARG, f"{what}: {why}")
+
+
+def _in(what: str, t: Optional[torch.Tensor], dtype, shape, dev: int) -> int:
+    """Address of a contiguous tensor (0 for None) once its type, shape and device are what the call takes."""
     if t is None:
         return 0
-    if not t.is_cuda or t.device.index != torch.cuda.current_device():
-        raise SplitLoraError(ERR_ARG, f"{what}: on {t.device}, not on the current CUDA device")
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise SplitLoraError(ERR_ARG, f"{what}: {t.dtype} {tuple(t.shape)}, not {dtype} {tuple(shape)}")
-    if codes:       # rows of codes may lie further apart than they are wide
-        if (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
-            raise SplitLoraError(ERR_ARG, f"{what}: strides {t.stride()}")
-    elif not t.is_contiguous():
-        raise SplitLoraError(ERR_ARG, f"{what}: not contiguous")
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != dev or not t.is_contiguous():
+        _refuse(what, t, dtype, shape, dev)
     return t.data_ptr()
 
 
-def _ld(codes: torch.Tensor) -> int:
-    return codes.stride(0) if codes.shape[0] > 1 else (codes.shape[1] + 15) // 16 * 16     # one row: any distance will do
+def _codes_in(what: str, t: torch.Tensor, M: int, d: int, dev: int):
+    """Address of int8 [M, d] and the distance of its rows, which may lie further apart than they are wide."""
+    if t.dtype is not _I8 or t.shape != (M, d) or t.get_device() != dev:
+        _refuse(what, t, _I8, (M, d), dev)
+    ld, one = t.stride()
+    if M == 1:
+        ld = (d + 15) // 16 * 16            # one row: any distance will do
+    if (one != 1 and d > 1) or ld < d:
+        _refuse(what, t, _I8, (M, d), dev)
+    return t.data_ptr(), ld
 
 
-def _rows(what: str, x: torch.Tensor):
-    """(dtype id, M, d) of a matrix of activations."""
-    if x.dim() != 2 or x.dtype not in (torch.bfloat16, torch.float32):
+def _matrix(what: str, x: torch.Tensor):
+    """(dtype id, M, d, device) of a matrix of activations on the current device."""
+    dt = _DTYPE_ID.get(x.dtype)
+    if dt is None or x.dim() != 2:
         raise SplitLoraError(ERR_ARG, f"{what}: {x.dtype} of {x.dim()} dimensions, not a float32 or bfloat16 matrix")
-    return _dt(x), x.shape[0], x.shape[1]
+    dev = torch.cuda.current_device()
+    M, d = x.shape
+    if x.get_device() != dev:
+        _refuse(what, x, x.dtype, x.shape, dev)
+    return dt, M, d, dev
 
 
 def empty_codes(M: int, d: int) -> torch.Tensor:
     """int8 [M, d] whose rows start on 16-byte boundaries (what lets linear_i8 run on the tensor cores)."""
     ld = (d + 15) // 16 * 16
-    t = torch.empty(M, ld, dtype=torch.int8, device="cuda")
+    t = torch.empty((M, ld), dtype=_I8, device="cuda")
     return t if ld == d else t[:, :d]
 
 
 def quantize_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
                   scales: Optional[torch.Tensor] = None):
     """x [M, d] -> (codes int8 [M, d], scales fp32 [M]); col_scale fp32 [d] multiplies x first (splitlora_quantize_rows)."""
-    dt, M, d = _rows("x", x)
+    dt, M, d, dev = _matrix("x", x)
     if codes is None:
         codes = empty_codes(M, d)
     if scales is None:
-        scales = torch.empty(M, dtype=torch.float32, device="cuda")
-    _rc(load().splitlora_quantize_rows(
-        dt, C.c_void_p(_arg("x", x, x.dtype, (M, d))), C.c_void_p(_arg("col_scale", col_scale, torch.float32, (d,))), C.c_int64(M), d,
-        C.c_void_p(_arg("codes", codes, torch.int8, (M, d), True)), C.c_int64(_ld(codes)),
-        C.c_void_p(_arg("scales", scales, torch.float32, (M,))), _stream_ptr()), "quantize_rows")
+        scales = torch.empty((M,), dtype=_F32, device=dev)
+    cp, ld = _codes_in("codes", codes, M, d, dev)
+    rc = load().splitlora_quantize_rows(dt, _in("x", x, x.dtype, (M, d), dev), _in("col_scale", col_scale, _F32, (d,), dev), M, d, cp, ld,
+                                        _in("scales", scales, _F32, (M,), dev), _raw_stream(dev))
+    if rc:
+        _rc(rc, "quantize_rows")
     return codes, scales
 
 
 def dequantize_rows(codes: torch.Tensor, scales: torch.Tensor, dtype=torch.bfloat16, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """codes [M, d] * scales [M] as `dtype` (splitlora_dequantize_rows)."""
-    M, d = codes.shape
+    if codes.dim() != 2:
+        raise SplitLoraError(ERR_ARG, "codes is a matrix")
     if out is None:
-        out = torch.empty(M, d, dtype=dtype, device="cuda")
-    dt, _, _ = _rows("out", out)
-    _rc(load().splitlora_dequantize_rows(
-        dt, C.c_void_p(_arg("codes", codes, torch.int8, (M, d), True)), C.c_int64(_ld(codes)),
-        C.c_void_p(_arg("scales", scales, torch.float32, (M,))), C.c_int64(M), d, C.c_void_p(_arg("out", out, out.dtype, (M, d))),
-        _stream_ptr()), "dequantize_rows")
+        out = torch.empty(codes.shape, dtype=dtype, device="cuda")
+    dt, M, d, dev = _matrix("out", out)
+    cp, ld = _codes_in("codes", codes, M, d, dev)
+    rc = load().splitlora_dequantize_rows(dt, cp, ld, _in("scales", scales, _F32, (M,), dev), M, d, _in("out", out, out.dtype, (M, d), dev),
+                                          _raw_stream(dev))
+    if rc:
+        _rc(rc, "dequantize_rows")
     return out
 
 
@@ -539,20 +575,22 @@ def rmsnorm_quantize(x: torch.Tensor, g: torch.Tensor, residual: Optional[torch.
                      h: Optional[torch.Tensor] = None, y: Optional[torch.Tensor] = None):
     """RMSNorm of x + residual as int8 codes (splitlora_rmsnorm_quantize): (codes, scales, h, y).  h is the sum (None without a
     residual, unless a buffer is passed), y the normalised row in x's dtype (None unless want_y or a buffer is passed)."""
-    dt, M, d = _rows("x", x)
+    dt, M, d, dev = _matrix("x", x)
+    t = x.dtype
     if codes is None:
         codes = empty_codes(M, d)
     if scales is None:
-        scales = torch.empty(M, dtype=torch.float32, device="cuda")
+        scales = torch.empty((M,), dtype=_F32, device=dev)
     if h is None and residual is not None:
         h = torch.empty_like(x)
     if y is None and want_y:
         y = torch.empty_like(x)
-    _rc(load().splitlora_rmsnorm_quantize(
-        dt, C.c_void_p(_arg("x", x, x.dtype, (M, d))), C.c_void_p(_arg("residual", residual, x.dtype, (M, d))),
-        C.c_void_p(_arg("g", g, x.dtype, (d,))), C.c_float(eps), C.c_int64(M), d, C.c_void_p(_arg("h", h, x.dtype, (M, d))),
-        C.c_void_p(_arg("y", y, x.dtype, (M, d))), C.c_void_p(_arg("codes", codes, torch.int8, (M, d), True)), C.c_int64(_ld(codes)),
-        C.c_void_p(_arg("scales", scales, torch.float32, (M,))), _stream_ptr()), "rmsnorm_quantize")
+    cp, ld = _codes_in("codes", codes, M, d, dev)
+    rc = load().splitlora_rmsnorm_quantize(
+        dt, _in("x", x, t, (M, d), dev), _in("residual", residual, t, (M, d), dev), _in("g", g, t, (d,), dev), eps, M, d,
+        _in("h", h, t, (M, d), dev), _in("y", y, t, (M, d), dev), cp, ld, _in("scales", scales, _F32, (M,), dev), _raw_stream(dev))
+    if rc:
+        _rc(rc, "rmsnorm_quantize")
     return codes, scales, h, y
 
 
@@ -560,23 +598,25 @@ def rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, g: torch.Tensor, resid: Optio
                 want_dg: bool = False, dx: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
     """Gradient of rmsnorm_quantize with respect to x (= residual) and, where want_dg, to g in fp32: (dx, dg or None)
     (splitlora_rmsnorm_bwd); resid: the gradient that reaches h by itself."""
-    dt, M, d = _rows("h", h)
+    dt, M, d, dev = _matrix("h", h)
+    t = h.dtype
     if dx is None:
         dx = torch.empty_like(h)
-    dg, ws_bytes = None, 0
+    dg, dgp, wsp, ws_bytes = None, 0, 0, 0
     if want_dg:
-        dg = torch.empty(d, dtype=torch.float32, device="cuda")
+        dg = torch.empty((d,), dtype=_F32, device=dev)
+        dgp = dg.data_ptr()
         if workspace is None:
             n = C.c_size_t(0)
-            _rc(load().splitlora_rmsnorm_bwd_workspace_bytes(C.c_int64(M), d, C.byref(n)), "rmsnorm_bwd_workspace_bytes")
-            workspace = torch.empty(n.value, dtype=torch.uint8, device="cuda")
+            _rc(load().splitlora_rmsnorm_bwd_workspace_bytes(M, d, C.byref(n)), "rmsnorm_bwd_workspace_bytes")
+            workspace = torch.empty((n.value,), dtype=torch.uint8, device=dev)
+        wsp = _in("workspace", workspace, workspace.dtype, workspace.shape, dev)
         ws_bytes = workspace.numel() * workspace.element_size()
-    _rc(load().splitlora_rmsnorm_bwd(
-        dt, C.c_void_p(_arg("dy", dy, h.dtype, (M, d))), C.c_void_p(_arg("h", h, h.dtype, (M, d))), C.c_void_p(_arg("g", g, h.dtype, (d,))),
-        C.c_void_p(_arg("resid", resid, h.dtype, (M, d))), C.c_float(eps), C.c_int64(M), d, C.c_void_p(_arg("dx", dx, h.dtype, (M, d))),
-        C.c_void_p(0 if dg is None else dg.data_ptr()),
-        C.c_void_p(0 if dg is None else _arg("workspace", workspace, workspace.dtype, workspace.shape)), C.c_size_t(ws_bytes),
-        _stream_ptr()), "rmsnorm_bwd")
+    rc = load().splitlora_rmsnorm_bwd(
+        dt, _in("dy", dy, t, (M, d), dev), _in("h", h, t, (M, d), dev), _in("g", g, t, (d,), dev), _in("resid", resid, t, (M, d), dev), eps, M, d,
+        _in("dx", dx, t, (M, d), dev), dgp, wsp, ws_bytes, _raw_stream(dev))
+    if rc:
+        _rc(rc, "rmsnorm_bwd")
     return dx, dg
 
 
@@ -590,14 +630,16 @@ def linear_i8(x: torch.Tensor, x_scales: torch.Tensor, W: torch.Tensor, w_scales
     M, K = x.shape
     N = W.shape[0]
     if y is None:
-        y = torch.empty(M, N, dtype=dtype, device="cuda")
-    dt, _, _ = _rows("y", y)
-    _rc(load().splitlora_linear_i8(
-        dt, C.c_void_p(_arg("x", x, torch.int8, (M, K), True)), C.c_int64(_ld(x)), C.c_void_p(_arg("x_scales", x_scales, torch.float32, (M,))),
-        C.c_void_p(_arg("W", W, torch.int8, (N, K), True)), C.c_int64(_ld(W)),
-        C.c_void_p(_arg("w_scales", w_scales, torch.float32, (N,))), C.c_void_p(_arg("bias", bias, y.dtype, (N,))),
-        C.c_void_p(_arg("residual", residual, y.dtype, (M, N))), M, K, N, C.c_void_p(_arg("y", y, y.dtype, (M, N))), _stream_ptr()),
-        "linear_i8")
+        y = torch.empty((M, N), dtype=dtype, device="cuda")
+    dt, _, _, dev = _matrix("y", y)
+    t = y.dtype
+    xp, ldx = _codes_in("x", x, M, K, dev)
+    wp, ldw = _codes_in("W", W, N, K, dev)
+    rc = load().splitlora_linear_i8(
+        dt, xp, ldx, _in("x_scales", x_scales, _F32, (M,), dev), wp, ldw, _in("w_scales", w_scales, _F32, (N,), dev), _in("bias", bias, t, (N,), dev),
+        _in("residual", residual, t, (M, N), dev), M, K, N, _in("y", y, t, (M, N), dev), _raw_stream(dev))
+    if rc:
+        _rc(rc, "linear_i8")
     return y
 
 
@@ -607,19 +649,19 @@ def distill_loss(logits: torch.Tensor, top_idx: torch.Tensor, top_logits: torch.
     """Loss against a teacher's top logits (top_idx int32, top_logits fp32 [M, k]) and labels int32 [M], with its gradient:
     (loss, a scalar on the device, row_loss [M], dlogits like logits) (splitlora_distill_loss).  vocab: columns of logits [M, ld] in use
     (default: all); dlogits may be logits."""
-    dt, M, ld = _rows("logits", logits)
+    dt, M, ld, dev = _matrix("logits", logits)
     if top_idx.dim() != 2:
         raise SplitLoraError(ERR_ARG, "top_idx is a matrix [M, k]")
     k = top_idx.shape[1]
+    t = logits.dtype
     if dlogits is None:
         dlogits = torch.empty_like(logits)
-    out = torch.empty(M + 2, dtype=torch.float32, device="cuda")       # row losses, loss, count
+    out = torch.empty((M + 2,), dtype=_F32, device=dev)       # row losses, loss, count
     p = out.data_ptr()
-    _rc(load().splitlora_distill_loss(
-        dt, C.c_void_p(_arg("logits", logits, logits.dtype, (M, ld))), C.c_int64(ld),
-        C.c_void_p(_arg("labels", labels, torch.int32, (M,))), C.c_void_p(_arg("top_idx", top_idx, torch.int32, (M, k))),
-        C.c_void_p(_arg("top_logits", top_logits, torch.float32, (M, k))), M, ld if vocab is None else int(vocab), k, C.c_float(temperature),
-        C.c_float(ce_weight), C.c_float(kd_weight), C.c_int64(normalizer),
-        C.c_void_p(_arg("dlogits", dlogits, logits.dtype, (M, ld))), C.c_int64(ld), C.c_void_p(p), C.c_void_p(p + 4 * M), C.c_void_p(p + 4 * M + 4),
-        _stream_ptr()), "distill_loss")
+    rc = load().splitlora_distill_loss(
+        dt, _in("logits", logits, t, (M, ld), dev), ld, _in("labels", labels, _I32, (M,), dev), _in("top_idx", top_idx, _I32, (M, k), dev),
+        _in("top_logits", top_logits, _F32, (M, k), dev), M, ld if vocab is None else int(vocab), k, temperature, ce_weight, kd_weight, normalizer,
+        _in("dlogits", dlogits, t, (M, ld), dev), ld, p, p + 4 * M, p + 4 * M + 4, _raw_stream(dev))
+    if rc:
+        _rc(rc, "distill_loss")
     return out[M], out[:M], dlogits

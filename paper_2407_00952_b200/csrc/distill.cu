@@ -12,6 +12,7 @@
 #include "host_common.h"
 #include "kernels.h"
 #include "launch.cuh"
+#include "tc_common.cuh"
 
 namespace sl {
 namespace {
@@ -34,8 +35,17 @@ struct DistillArgs {
   int V, k;
   float temp, wc, wk;
   float c1, cT;            // log2(e) / temperature of the first and second exponential
-  float* rows; const int* n_valid; int n_fixed;
+  float* rows; int* n_valid; int n_fixed;
+  int same;                // rows of logits and gradient start at the same place of a 16-byte vector
+  int count_here;          // the ring kernel counts the labels and leaves the count in n_valid
 };
+
+template <typename T> __device__ __forceinline__ void store_vec(T* p, const float* v) {
+  Vec16<T> o;
+#pragma unroll
+  for (int i = 0; i < Vec16<T>::N; ++i) o.set(i, v[i]);
+  o.store(p);
+}
 
 // Running maximum and sums of exponentials relative to it.
 struct Online { float m, s1, sT; };
@@ -226,6 +236,306 @@ distill_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p
   }
 }
 
+// ------------------------------------------------------------------------------------------
+// rows in shared memory
+// ------------------------------------------------------------------------------------------
+// Persistent blocks walk the rows.  One thread copies the next rows into a ring of one or two buffers with bulk copies; a row's
+// logits are read from there twice (maximum, exponentials), the exponentials of a temperature stay in registers until the
+// row's sums are known, and the gradient leaves from there: a logit costs HBM one read and one write, and one exponential where
+// one temperature is enough or the two are 1 and 2 (then e^z = (e^(z/2))^2).  What bounds the streaming kernel above is the
+// exponential unit and instruction issue (4 exponentials per logit) as much as traffic.
+// Rows may start anywhere (a vocabulary of 50257 entries in contiguous rows): a row is held as the 16-byte vectors that cover it, its
+// first and last vector patched by the threads that own them; the copies take whole vectors inside the buffer and plain
+// loads the ragged ends of the first and last row.
+enum { EXP_HALF = 2 };   // temperatures 1 and 2
+
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// E: logits per thread; MINB: blocks per SM.
+template <typename T, int E, int THREADS, int MINB, int MODE>
+__global__ void __launch_bounds__(THREADS, MINB)
+distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p, int M, int nbuf, int buf_bytes, int* status) {
+  constexpr int W = Vec16<T>::N, NV = E / W, NW = THREADS / 32;
+  extern __shared__ __align__(128) uint8_t smem[];       // nbuf rows
+  __shared__ __align__(16) int sh_idx[2][DISTILL_MAX_K];
+  __shared__ __align__(16) float sh_q[2][DISTILL_MAX_K], sh_z[2][DISTILL_MAX_K];
+  __shared__ float sh_m[2][32], sh_sT[2][32], sh_s1[2][32], sh_zy[2];
+  __shared__ __align__(8) uint64_t bars[2];
+  __shared__ int sh_teach[2], sh_count[32], sh_abort;
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const int V = p.V, k = p.k;
+  const uint32_t smem_base = tc::smem_u32(smem);
+  if (tid == 0) {
+    tc::mbar_init(tc::smem_u32(&bars[0]), 1);
+    tc::mbar_init(tc::smem_u32(&bars[1]), 1);
+    sh_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  }
+  __syncthreads();
+  overlap_sync();
+
+  auto label_of = [&](int64_t r) { return p.labels && r < M ? p.labels[r] : 0; };
+  auto takes_part = [&](int y) { return y >= 0 && y < V; };
+  // thread 0: the next row that takes part into the next buffer
+  int64_t ahead = blockIdx.x;
+  int issued = 0;
+  auto issue_next = [&]() {
+    while (ahead < M && !takes_part(label_of(ahead))) ahead += gridDim.x;
+    if (ahead >= M) return;
+    const int b = issued % nbuf;
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(logits + ahead * p.ld), a1 = a0 + (uintptr_t)V * sizeof(T), f0 = a0 & ~(uintptr_t)15;
+    const uintptr_t lo = ahead == 0 && f0 < a0 ? f0 + 16 : f0, hi = ahead == M - 1 ? a1 & ~(uintptr_t)15 : (a1 + 15) & ~(uintptr_t)15;
+    const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) : 0u, bar = tc::smem_u32(&bars[b]);
+    tc::mbar_expect_tx(bar, bytes);
+    if (bytes)
+      asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                   ::"r"(smem_base + (uint32_t)(b * buf_bytes) + (uint32_t)(lo - f0)), "l"(lo), "r"(bytes), "r"(bar) : "memory");
+    ++issued;
+    ahead += gridDim.x;
+  };
+  // warp 0: a row's teacher entries into the tables, one row ahead; lane j % 32 copies entry j and reads it
+  auto fetch_teacher = [&](int64_t r, int par) {
+    if (r < M)
+      for (int j = lane; j < k; j += 32) {
+        cp_async4(tc::smem_u32(&sh_idx[par][j]), p.idx + r * k + j);
+        cp_async4(tc::smem_u32(&sh_q[par][j]), p.t + r * k + j);
+      }
+  };
+  if (tid == 0)
+    for (int b = 0; b < nbuf; ++b) issue_next();
+  if (warp == 0) fetch_teacher(blockIdx.x, 0);
+  int n = p.n_fixed;
+  if (p.n_valid && !p.count_here) n = *p.n_valid;
+  if (p.count_here) {                      // few labels: every block counts them itself
+    int c = 0;
+    for (int i = tid; i < M; i += THREADS) c += takes_part(p.labels[i]) ? 1 : 0;
+    c = __reduce_add_sync(0xffffffffu, c);
+    if (lane == 0) sh_count[warp] = c;
+    __syncthreads();
+    n = 0;
+    for (int w = 0; w < NW; ++w) n += sh_count[w];
+    if (blockIdx.x == 0 && tid == 0) *p.n_valid = n;
+  }
+  const float inv_n = 1.0f / (float)(n > 0 ? n : 1), inv_t = 1.0f / p.temp;
+
+  int done = 0, par = 0;                   // rows that took part; tables of this row
+  int y_next = label_of(blockIdx.x);
+  for (int64_t row = blockIdx.x; row < M; row += gridDim.x) {
+    const int y = y_next;
+    y_next = label_of(row + gridDim.x);
+    const int s = (int)((reinterpret_cast<uintptr_t>(logits + row * p.ld) & 15u) / sizeof(T));
+    T* out = grad + row * p.ldo - s;       // position q = s + column
+    const int end = s + V, out_end = s + (int)p.ldo, nvec = (end + W - 1) / W, last = nvec - 1;
+    if (warp == 0) asm volatile("cp.async.wait_all;" ::: "memory");
+    // positions [from, to) of the gradient become zero
+    auto zeros = [&](int from, int to) {
+      for (int v = from / W + tid; v * W < to; v += THREADS) {
+        if (p.same && v * W >= from && (v + 1) * W <= to) *reinterpret_cast<uint4*>(out + (int64_t)v * W) = make_uint4(0u, 0u, 0u, 0u);
+        else
+          for (int i = 0; i < W; ++i)
+            if (v * W + i >= from && v * W + i < to) out[v * W + i] = from_f<T>(0.f);
+      }
+    };
+    if (!takes_part(y)) {
+      if (tid == 0) p.rows[row] = 0.f;
+      zeros(s, out_end);
+      if (warp == 0) fetch_teacher(row + gridDim.x, par);      // over this row's entries: the other tables may still be read
+      continue;
+    }
+    const int b = done % nbuf;
+    tc::mbar_wait(tc::smem_u32(&bars[b]), (uint32_t)(done / nbuf) & 1u, &sh_abort, status, 81);
+    T* zs = reinterpret_cast<T*>(smem + (size_t)b * buf_bytes);
+    // what lies outside the row in its first and last vector, by the threads that own them; in the first and last row also what the
+    // copies left out
+    const bool head_left = row == 0 && s > 0, tail_left = row == M - 1 && end % W != 0;
+    if ((tid == 0 && s > 0) || (tid == last % THREADS && end % W != 0)) {
+      const T* z = logits + row * p.ld - s;
+      if (tid == 0)
+        for (int q = 0; q < W; ++q) {
+          if (q < s) zs[q] = from_f<T>(-INFINITY);
+          else if (q < end && (head_left || (tail_left && last == 0))) zs[q] = z[q];
+        }
+      if (tid == last % THREADS)
+        for (int q = last * W; q < nvec * W; ++q) {
+          if (q >= end) zs[q] = from_f<T>(-INFINITY);
+          else if (q >= s && (tail_left || (head_left && last == 0))) zs[q] = z[q];
+        }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // before a copy takes the buffer again
+    }
+    // ---- this thread's maximum, then its exponentials relative to it
+    float m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int v = j * THREADS + tid;
+      if (v < nvec) {
+        Vec16<T> r; r.load(zs + (size_t)v * W);
+        if constexpr (W == 8) {
+          const __nv_bfloat162* h2 = reinterpret_cast<const __nv_bfloat162*>(&r.raw);
+          const __nv_bfloat162 m2 = __hmax2(__hmax2(h2[0], h2[1]), __hmax2(h2[2], h2[3]));
+          m = fmaxf(m, fmaxf(__low2float(m2), __high2float(m2)));
+        } else {
+#pragma unroll
+          for (int i = 0; i < W; ++i) m = fmaxf(m, r.get(i));
+        }
+      }
+    }
+    const bool none = m == -INFINITY;
+    const float mine = none ? 0.f : m;
+    float e[NV][W];
+    float sT = 0.f, s1 = 0.f;
+    const uint64_t one2 = tc::pack2(1.0f, 1.0f), cT2 = tc::pack2(p.cT, p.cT), neg2 = tc::pack2(-mine, -mine);
+    const uint64_t c12 = tc::pack2(p.c1, p.c1);
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int v = j * THREADS + tid;
+      if (v < nvec) {
+        Vec16<T> r; r.load(zs + (size_t)v * W);
+#pragma unroll
+        for (int i = 0; i < W; i += 2) {
+          const uint64_t dd = tc::fma2(tc::pack2(r.get(i), r.get(i + 1)), one2, neg2);      // z - maximum
+          float a, c;
+          tc::unpack2(tc::mul2(dd, cT2), a, c);
+          e[j][i] = ex2(a); e[j][i + 1] = ex2(c);
+          sT += e[j][i]; sT += e[j][i + 1];
+          if constexpr (MODE == EXP_HALF) { s1 = fmaf(e[j][i], e[j][i], s1); s1 = fmaf(e[j][i + 1], e[j][i + 1], s1); }
+          if constexpr (MODE == EXP_TWO) {
+            tc::unpack2(tc::mul2(dd, c12), a, c);
+            s1 += ex2(a); s1 += ex2(c);
+          }
+        }
+      }
+    }
+    // ---- warp 0: the teacher's distribution
+    float tsum = 0.f, tmax = -INFINITY;
+    if (warp == 0) {
+      const bool left = head_left || tail_left;          // another thread's patch may not be visible yet: the logits themselves
+      for (int j = lane; j < k; j += 32) {
+        const int v = sh_idx[par][j];
+        const bool ok = v >= 0 && v < V;
+        const float t = ok ? sh_q[par][j] : -INFINITY;
+        if (!ok) sh_idx[par][j] = -1;
+        sh_q[par][j] = t;
+        sh_z[par][j] = !ok ? 0.f : to_f<T>(left ? logits[row * p.ld + v] : zs[s + v]);
+        tmax = t != t || tmax != tmax ? __uint_as_float(0x7fffffffu) : fmaxf(tmax, t);
+      }
+      for (int j = k + lane; j < (k + 3) / 4 * 4; j += 32) sh_idx[par][j] = -1;
+      const bool nan = __any_sync(0xffffffffu, tmax != tmax);
+      tmax = nan ? __uint_as_float(0x7fffffffu) : warp_max(tmax);
+      for (int j = lane; j < k; j += 32) tsum += expf((sh_q[par][j] - tmax) * inv_t);       // not used where tmax is -inf
+      tsum = warp_sum(tsum);
+      if (lane == 0) {
+        sh_zy[par] = p.labels ? to_f<T>(left ? logits[row * p.ld + y] : zs[s + y]) : 0.f;
+        sh_teach[par] = tmax != -INFINITY && p.wk != 0.f;    // else the teacher says nothing about this row
+      }
+    }
+    // ---- the row's maximum and sums.  Without a maximum the sums are 0 or, from NaN, NaN: no factor
+    auto factor = [&](float from, float to, float c) { return from == -INFINITY ? 1.f : ex2((from - to) * c); };
+    const float wm = warp_max(m), wbase = wm == -INFINITY ? 0.f : wm;
+    {
+      const float f = factor(m, wbase, p.cT);
+      sT = warp_sum(sT * f);
+      if constexpr (MODE == EXP_HALF) s1 = warp_sum(s1 * (f * f));
+      if constexpr (MODE == EXP_TWO) s1 = warp_sum(s1 * factor(m, wbase, p.c1));
+    }
+    if (lane == 0) {
+      sh_m[par][warp] = wm; sh_sT[par][warp] = sT;
+      if constexpr (MODE != EXP_ONE) sh_s1[par][warp] = s1;
+    }
+    __syncthreads();
+    ++done;
+    if (MODE != EXP_TWO && tid == 0) issue_next();       // the logits are not read again
+    {
+      const float rm = lane < NW ? sh_m[par][lane] : -INFINITY;
+      m = warp_max(rm);
+      const float base = m == -INFINITY ? 0.f : m, f = factor(rm, base, p.cT);
+      sT = warp_sum(lane < NW ? sh_sT[par][lane] * f : 0.f);
+      if constexpr (MODE == EXP_HALF) s1 = warp_sum(lane < NW ? sh_s1[par][lane] * (f * f) : 0.f);
+      else if constexpr (MODE == EXP_TWO) s1 = warp_sum(lane < NW ? sh_s1[par][lane] * factor(rm, base, p.c1) : 0.f);
+      else s1 = sT;
+    }
+    const float base = m == -INFINITY ? 0.f : m;
+    const bool teach = sh_teach[par] != 0;
+    // ---- warp 0: the divergence and the row's loss
+    if (warp == 0) {
+      const float log_s1 = logf(s1), log_sT = logf(sT), log_ts = logf(tsum);
+      float kl = 0.f;
+      for (int j = lane; j < k; j += 32) {
+        const float lq = (sh_q[par][j] - tmax) * inv_t - log_ts;
+        const float q = teach ? expf(lq) : 0.f;
+        if (q != 0.f) kl += q * fmaf(p.temp, lq + log_sT, base - sh_z[par][j]);      // T times the divergence: (z - base) / T could overflow
+        sh_q[par][j] = q;
+      }
+      kl = warp_sum(kl);
+      if (lane == 0) {
+        float r = teach ? p.wk * p.temp * kl : 0.f;
+        if (p.wc != 0.f) r += p.wc * (log_s1 - (sh_zy[par] - base));
+        p.rows[row] = r;
+      }
+      fetch_teacher(row + gridDim.x, par ^ 1);
+    }
+    // ---- gradient
+    const float wkT = teach ? p.wk * p.temp : 0.f;
+    const float f1 = MODE == EXP_ONE ? (p.wc + wkT) / s1 * inv_n : p.wc / s1 * inv_n, fT = MODE == EXP_ONE ? 0.f : wkT / sT * inv_n;
+    // of this thread's exponentials, which are relative to its own maximum
+    const float up = none ? 1.f : ex2((mine - base) * p.cT);           // (a thread of -inf alone has exponentials of 0)
+    const float g1 = MODE == EXP_ONE ? f1 * up : MODE == EXP_HALF ? f1 * (up * up) : f1, gT = fT * up;
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+      const int v = j * THREADS + tid;
+      if (v < nvec) {
+        float o[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+          if constexpr (MODE == EXP_ONE) o[i] = e[j][i] * g1;
+          if constexpr (MODE == EXP_HALF) o[i] = e[j][i] * fmaf(e[j][i], g1, gT);
+        }
+        if constexpr (MODE == EXP_TWO) {
+          Vec16<T> r; r.load(zs + (size_t)v * W);
+#pragma unroll
+          for (int i = 0; i < W; ++i) o[i] = fmaf(e[j][i], gT, g1 * ex2((r.get(i) - base) * p.c1));
+        }
+        if (p.same && v * W >= s && (v + 1) * W <= end) {
+          store_vec<T>(out + (int64_t)v * W, o);
+        } else {
+#pragma unroll
+          for (int i = 0; i < W; ++i)
+            if (v * W + i >= s && v * W + i < end) out[v * W + i] = from_f<T>(o[i]);
+        }
+      }
+    }
+    if (out_end > end) zeros(end, out_end);
+    __syncthreads();
+    if (MODE == EXP_TWO && tid == 0) issue_next();
+    // ---- the entries with a target, from the last threads on: the first entry of an index writes for all of them
+    auto value = [&](float z) {
+      if constexpr (MODE == EXP_TWO) return fmaf(f1, ex2((z - base) * p.c1), fT * ex2((z - base) * p.cT));
+      const float x = ex2((z - base) * p.cT);
+      return MODE == EXP_ONE ? f1 * x : x * fmaf(x, f1, fT);
+    };
+    for (int j = THREADS - 1 - tid; j <= k; j += THREADS) {
+      const int v = j < k ? sh_idx[par][j] : p.labels ? y : -1;        // entry k: the label
+      if (v < 0) continue;
+      bool first = true;
+      float q = 0.f;
+      for (int i = 0; i < k; i += 4) {
+        const int4 w = *reinterpret_cast<const int4*>(&sh_idx[par][i]);
+        if (w.x == v) { if (i < j) first = false; q += sh_q[par][i]; }
+        if (w.y == v) { if (i + 1 < j) first = false; q += sh_q[par][i + 1]; }
+        if (w.z == v) { if (i + 2 < j) first = false; q += sh_q[par][i + 2]; }
+        if (w.w == v) { if (i + 3 < j) first = false; q += sh_q[par][i + 3]; }
+      }
+      if (!first) continue;
+      float r = value(j < k ? sh_z[par][j] : sh_zy[par]) - wkT * inv_n * q;
+      if (p.labels && v == y) r -= p.wc * inv_n;
+      out[s + v] = from_f<T>(r);
+    }
+    par ^= 1;
+  }
+}
+
 __global__ void distill_count_kernel(const int32_t* __restrict__ labels, int M, int V, int* __restrict__ n_valid) {
   overlap_sync();
   __shared__ int sh[32];
@@ -257,9 +567,45 @@ __global__ void distill_loss_kernel(const float* __restrict__ rows, int M, const
 
 }  // namespace
 
+namespace {
+
+// Rows up to this many labels are counted by every block of the ring kernel instead of a launch in front of it.
+constexpr int COUNT_HERE = 4096;
+constexpr int RING_MAX_VOCAB = 53248 - 7;              // the widest block: 512 threads x 104 logits, at any alignment
+constexpr int RING_TABLES = 8192, RING_BYTES = 232448 - 1024 - RING_TABLES;     // static tables; dynamic shared memory of all blocks of an SM
+
+template <typename T, int E, int THREADS, int MINB, int MODE>
+cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, int* status, cudaStream_t st) {
+  const auto kernel = distill_ring_kernel<T, E, THREADS, MINB, MODE>;
+  static PerDeviceOnce once;
+  const int dev = current_device();
+  if (once.needed(dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, RING_BYTES);
+    if (e != cudaSuccess) return e;
+    once.done(dev);
+  }
+  const int buf = (int)(((size_t)p.V * sizeof(T) + 15) / 16 * 16 + 16), nbuf = 2 * buf <= RING_BYTES ? 2 : 1;
+  const int fit = (RING_BYTES + RING_TABLES) / (nbuf * buf + RING_TABLES), per_sm = fit < MINB ? fit : MINB;
+  const int64_t most = (int64_t)num_sms() * per_sm;
+  return launch_overlapped(kernel, dim3((unsigned)(M < most ? M : most)), dim3(THREADS), (size_t)nbuf * buf, st, logits, grad, p, M, nbuf, buf, status);
+}
+
+// The smallest block whose registers hold a row.
+template <typename T, int MODE>
+cudaError_t ring(const T* logits, T* grad, const DistillArgs& p, int M, int* status, cudaStream_t st) {
+  const int need = p.V + Vec16<T>::N - 1;              // at any alignment
+  if (need <= 2048) return launch_ring<T, 16, 128, 8, MODE>(logits, grad, p, M, status, st);
+  if (need <= 8192) return launch_ring<T, 64, 128, 4, MODE>(logits, grad, p, M, status, st);
+  if (need <= 16384) return launch_ring<T, 64, 256, 2, MODE>(logits, grad, p, M, status, st);
+  if (need <= 32768) return launch_ring<T, 64, 512, 1, MODE>(logits, grad, p, M, status, st);
+  return launch_ring<T, 104, 512, 1, MODE>(logits, grad, p, M, status, st);
+}
+
+}  // namespace
+
 cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* labels, const int32_t* idx, const float* t, int M, int V, int k,
                     float temperature, float wc, float wk, int normalizer, void* grad, int64_t ldo, float* rows, int* n_valid, float* loss,
-                    cudaStream_t st) {
+                    int* status, cudaStream_t st) {
   DistillArgs p;
   p.labels = labels; p.idx = idx; p.t = t; p.ld = ld; p.ldo = ldo; p.V = V; p.k = k; p.temp = temperature; p.wc = wc; p.wk = wk; p.rows = rows;
   const bool count = labels != nullptr && normalizer <= 0;
@@ -267,20 +613,29 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
   p.n_fixed = normalizer > 0 ? normalizer : M;
   const bool two = wc != 0.f && wk != 0.f && temperature != 1.0f;
   // EXP_ONE: the temperature of the term that has a weight
-  p.cT = LOG2E / temperature;
-  p.c1 = two || wk == 0.f ? LOG2E : p.cT;
+  p.cT = two || wk != 0.f ? LOG2E / temperature : LOG2E;
+  p.c1 = two ? LOG2E : p.cT;
+  p.count_here = 0;
   cudaError_t e = cudaSuccess;
-  if (count) {
+  const size_t es = dtype_size(dt);
+  p.same = ((reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(grad)) & 15u) == 0 && ((ld - ldo) * (int64_t)es) % 16 == 0;
+  const bool in_ring = V <= RING_MAX_VOCAB;
+  p.count_here = in_ring && count && M <= COUNT_HERE;
+  if (count && !p.count_here) {
     e = launch_overlapped(distill_count_kernel, dim3(1), dim3(1024), 0, st, labels, M, V, n_valid);
     if (e != cudaSuccess) return e;
   }
   auto run = [&](auto type) -> cudaError_t {
     using T = decltype(type);
     constexpr int N = Vec16<T>::N;
+    const T* z = (const T*)logits;
+    T* g = (T*)grad;
+    if (in_ring) {
+      if (!two) return ring<T, EXP_ONE>(z, g, p, M, status, st);
+      return temperature == 2.0f ? ring<T, EXP_HALF>(z, g, p, M, status, st) : ring<T, EXP_TWO>(z, g, p, M, status, st);
+    }
     const bool vec = ld % N == 0 && ldo % N == 0 && ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(grad)) & 15u) == 0;
-    auto go = [&](auto kernel) -> cudaError_t {
-      return launch_overlapped(kernel, dim3((unsigned)M), dim3(256), 0, st, (const T*)logits, (T*)grad, p);
-    };
+    auto go = [&](auto kernel) -> cudaError_t { return launch_overlapped(kernel, dim3((unsigned)M), dim3(256), 0, st, z, g, p); };
     if (vec) return two ? go(distill_kernel<T, N, EXP_TWO>) : go(distill_kernel<T, N, EXP_ONE>);
     return two ? go(distill_kernel<T, 1, EXP_TWO>) : go(distill_kernel<T, 1, EXP_ONE>);
   };

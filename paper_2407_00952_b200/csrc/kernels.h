@@ -270,6 +270,6 @@ cudaError_t gemm_i8(const I8Args& a, int* status, cudaStream_t st);
 constexpr int DISTILL_MAX_K = 256;
 cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* labels, const int32_t* idx, const float* t, int M, int V, int k,
                     float temperature, float wc, float wk, int normalizer, void* grad, int64_t ldo, float* rows, int* n_valid, float* loss,
-                    cudaStream_t st);
+                    int* status, cudaStream_t st);
 
 }  // namespace sl

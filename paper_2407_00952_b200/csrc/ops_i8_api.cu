@@ -96,8 +96,10 @@ int splitlora_distill_loss(int dtype, const void* logits, int64_t ld, const int3
   if (!aligned_elem(dtype, logits) || !aligned_elem(dtype, dlogits)) return SPLITLORA_ERR_ALIGN;
   for (const void* p : {(const void*)labels, (const void*)top_idx, (const void*)top_logits, (const void*)row_loss, (const void*)loss, (const void*)n_valid})
     if (!aligned(p, 4)) return SPLITLORA_ERR_ALIGN;
+  int* status = library_status_word();
+  if (!status) return SPLITLORA_ERR_CUDA;
   return done(distill(dtype, logits, ld, labels, top_idx, top_logits, M, vocab, k, temperature, ce_weight, kd_weight, (int)normalizer, dlogits, ld_grad,
-                      row_loss, n_valid, loss, (cudaStream_t)stream));
+                      row_loss, n_valid, loss, status, (cudaStream_t)stream));
 }
 
 }  // extern "C"
