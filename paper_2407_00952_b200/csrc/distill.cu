@@ -35,16 +35,16 @@ struct DistillArgs {
   int V, k;
   float temp, wc, wk;
   float c1, cT;            // log2(e) / temperature of the first and second exponential
+  float inv_t, inv_n;      // inv_n: set by the kernel
   float* rows; int* n_valid; int n_fixed;
   int same;                // rows of logits and gradient start at the same place of a 16-byte vector
   int count_here;          // the ring kernel counts the labels and leaves the count in n_valid
 };
 
-template <typename T> __device__ __forceinline__ void store_vec(T* p, const float* v) {
-  Vec16<T> o;
+// one by one, where the gradient's rows start at another place of a 16-byte vector (out of line: the loop around it is unrolled)
+template <typename T> __device__ __noinline__ void store_each(T* p, Vec16<T> o) {
 #pragma unroll
-  for (int i = 0; i < Vec16<T>::N; ++i) o.set(i, v[i]);
-  o.store(p);
+  for (int i = 0; i < Vec16<T>::N; ++i) p[i] = reinterpret_cast<const T*>(&o.raw)[i];
 }
 
 // Running maximum and sums of exponentials relative to it.
@@ -253,17 +253,32 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// E: logits per thread; MINB: blocks per SM.
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// the W values of a 16-byte vector as W / 2 packed pairs
+__device__ __forceinline__ uint64_t pair_of(const Vec16<bf16>& r, int i) { return tc::bf16x2_to_f32x2(reinterpret_cast<const uint32_t*>(&r.raw)[i]); }
+__device__ __forceinline__ uint64_t pair_of(const Vec16<float>& r, int i) { return tc::pack2(r.get(2 * i), r.get(2 * i + 1)); }
+
+constexpr int SLOTS = 3;   // rows whose tables are in use at once: the next one's, this one's, the one whose targets are being written
+
+// E: logits per thread; MINB: blocks per SM.  One barrier per row: behind it every logit of the row has been read, every sum is
+// there, and the previous row's gradient has been written but for the entries with a target, which follow then.
 template <typename T, int E, int THREADS, int MINB, int MODE>
 __global__ void __launch_bounds__(THREADS, MINB)
 distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p, int M, int nbuf, int buf_bytes, int* status) {
-  constexpr int W = Vec16<T>::N, NV = E / W, NW = THREADS / 32;
+  constexpr int W = Vec16<T>::N, NV = E / W, NW = THREADS / 32, ISSUER = THREADS - 32;
   extern __shared__ __align__(128) uint8_t smem[];       // nbuf rows
-  __shared__ __align__(16) int sh_idx[2][DISTILL_MAX_K];
-  __shared__ __align__(16) float sh_q[2][DISTILL_MAX_K], sh_z[2][DISTILL_MAX_K];
-  __shared__ float sh_m[2][32], sh_sT[2][32], sh_s1[2][32], sh_zy[2];
+  __shared__ __align__(16) int sh_idx[SLOTS][DISTILL_MAX_K];
+  __shared__ float sh_q[SLOTS][DISTILL_MAX_K], sh_z[SLOTS][DISTILL_MAX_K];
+  __shared__ float sh_m[2][32], sh_sT[2][32], sh_s1[2][32];
+  __shared__ T sh_edge[2][2][W];                         // logits of the row's ragged first and last vector
+  __shared__ float sh_zy[SLOTS], sh_f1[SLOTS], sh_fT[SLOTS], sh_base[SLOTS], sh_fq[SLOTS];
+  __shared__ int64_t sh_row[SLOTS];
+  __shared__ int sh_y[SLOTS], sh_teach[SLOTS], sh_count[32], sh_abort;
   __shared__ __align__(8) uint64_t bars[2];
-  __shared__ int sh_teach[2], sh_count[32], sh_abort;
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int V = p.V, k = p.k;
   const uint32_t smem_base = tc::smem_u32(smem);
@@ -279,7 +294,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
 
   auto label_of = [&](int64_t r) { return p.labels && r < M ? p.labels[r] : 0; };
   auto takes_part = [&](int y) { return y >= 0 && y < V; };
-  // thread 0: the next row that takes part into the next buffer
+  // thread ISSUER: the next row that takes part into the next buffer
   int64_t ahead = blockIdx.x;
   int issued = 0;
   auto issue_next = [&]() {
@@ -297,14 +312,39 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
     ahead += gridDim.x;
   };
   // warp 0: a row's teacher entries into the tables, one row ahead; lane j % 32 copies entry j and reads it
-  auto fetch_teacher = [&](int64_t r, int par) {
+  auto fetch_teacher = [&](int64_t r, int slot) {
     if (r < M)
       for (int j = lane; j < k; j += 32) {
-        cp_async4(tc::smem_u32(&sh_idx[par][j]), p.idx + r * k + j);
-        cp_async4(tc::smem_u32(&sh_q[par][j]), p.t + r * k + j);
+        cp_async4(tc::smem_u32(&sh_idx[slot][j]), p.idx + r * k + j);
+        cp_async4(tc::smem_u32(&sh_q[slot][j]), p.t + r * k + j);
       }
   };
-  if (tid == 0)
+  // from warp 2 on: the entries of the row in `slot` that carry a target; the first entry of an index writes for all of them
+  auto write_targets = [&](int slot) {
+    const float f1 = sh_f1[slot], fT = sh_fT[slot], base = sh_base[slot];
+    const int y = sh_y[slot];
+    T* out = grad + sh_row[slot] * p.ldo;
+    for (int j = tid - 64; j <= k; j += THREADS - 64) {
+      const int v = j < k ? sh_idx[slot][j] : y;         // entry k: the label (-1: no labels)
+      if (v < 0) continue;
+      bool first = true;
+      float q = 0.f;
+      for (int i = 0; i < k; i += 4) {
+        const int4 w = *reinterpret_cast<const int4*>(&sh_idx[slot][i]);
+        if (w.x == v) { if (i < j) first = false; q += sh_q[slot][i]; }
+        if (w.y == v) { if (i + 1 < j) first = false; q += sh_q[slot][i + 1]; }
+        if (w.z == v) { if (i + 2 < j) first = false; q += sh_q[slot][i + 2]; }
+        if (w.w == v) { if (i + 3 < j) first = false; q += sh_q[slot][i + 3]; }
+      }
+      if (!first) continue;
+      const float z = (j < k ? sh_z[slot][j] : sh_zy[slot]) - base, x = ex2(z * p.cT);
+      float r = MODE == EXP_ONE ? f1 * x : MODE == EXP_HALF ? x * fmaf(x, f1, fT) : fmaf(f1, ex2(z * p.c1), fT * x);
+      r -= sh_fq[slot] * q;
+      if (v == y) r -= p.wc * p.inv_n;
+      out[v] = from_f<T>(r);
+    }
+  };
+  if (tid == ISSUER)
     for (int b = 0; b < nbuf; ++b) issue_next();
   if (warp == 0) fetch_teacher(blockIdx.x, 0);
   int n = p.n_fixed;
@@ -319,9 +359,9 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
     for (int w = 0; w < NW; ++w) n += sh_count[w];
     if (blockIdx.x == 0 && tid == 0) *p.n_valid = n;
   }
-  const float inv_n = 1.0f / (float)(n > 0 ? n : 1), inv_t = 1.0f / p.temp;
+  p.inv_n = 1.0f / (float)(n > 0 ? n : 1);
 
-  int done = 0, par = 0;                   // rows that took part; tables of this row
+  int done = 0, slot = 0;                  // rows that took part; tables of this row
   int y_next = label_of(blockIdx.x);
   for (int64_t row = blockIdx.x; row < M; row += gridDim.x) {
     const int y = y_next;
@@ -329,7 +369,6 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
     const int s = (int)((reinterpret_cast<uintptr_t>(logits + row * p.ld) & 15u) / sizeof(T));
     T* out = grad + row * p.ldo - s;       // position q = s + column
     const int end = s + V, out_end = s + (int)p.ldo, nvec = (end + W - 1) / W, last = nvec - 1;
-    if (warp == 0) asm volatile("cp.async.wait_all;" ::: "memory");
     // positions [from, to) of the gradient become zero
     auto zeros = [&](int from, int to) {
       for (int v = from / W + tid; v * W < to; v += THREADS) {
@@ -339,44 +378,51 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
             if (v * W + i >= from && v * W + i < to) out[v * W + i] = from_f<T>(0.f);
       }
     };
+    if (warp == 0) asm volatile("cp.async.wait_all;" ::: "memory");
     if (!takes_part(y)) {
       if (tid == 0) p.rows[row] = 0.f;
       zeros(s, out_end);
-      if (warp == 0) fetch_teacher(row + gridDim.x, par);      // over this row's entries: the other tables may still be read
+      if (warp == 0) fetch_teacher(row + gridDim.x, slot);     // over this row's entries: the other tables may still be read
       continue;
     }
-    const int b = done % nbuf;
+    const int b = done % nbuf, par = done & 1;
     tc::mbar_wait(tc::smem_u32(&bars[b]), (uint32_t)(done / nbuf) & 1u, &sh_abort, status, 81);
     T* zs = reinterpret_cast<T*>(smem + (size_t)b * buf_bytes);
-    // what lies outside the row in its first and last vector, by the threads that own them; in the first and last row also what the
-    // copies left out
-    const bool head_left = row == 0 && s > 0, tail_left = row == M - 1 && end % W != 0;
-    if ((tid == 0 && s > 0) || (tid == last % THREADS && end % W != 0)) {
+    // A ragged first or last vector (in the first and last row of all the copies left it out): the thread that owns it keeps its
+    // logits for the gradient and puts -inf around them.
+    const bool ragged_first = s > 0 || (last == 0 && end % W != 0), ragged_last = end % W != 0;
+    if ((tid == 0 && ragged_first) || (tid == last % THREADS && ragged_last)) {
       const T* z = logits + row * p.ld - s;
-      if (tid == 0)
-        for (int q = 0; q < W; ++q) {
-          if (q < s) zs[q] = from_f<T>(-INFINITY);
-          else if (q < end && (head_left || (tail_left && last == 0))) zs[q] = z[q];
-        }
-      if (tid == last % THREADS)
-        for (int q = last * W; q < nvec * W; ++q) {
-          if (q >= end) zs[q] = from_f<T>(-INFINITY);
-          else if (q >= s && (tail_left || (head_left && last == 0))) zs[q] = z[q];
+      const bool left = row == 0 || row == M - 1;
+      for (int which = tid == 0 && ragged_first ? 0 : 1; which < (tid == last % THREADS && ragged_last ? 2 : 1); ++which)
+        for (int i = 0; i < W; ++i) {
+          const int q = (which ? last * W : 0) + i;
+          const T v = q < s || q >= end ? from_f<T>(-INFINITY) : left ? z[q] : zs[q];
+          zs[q] = v;
+          sh_edge[par][which][i] = v;
         }
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // before a copy takes the buffer again
     }
     // ---- this thread's maximum, then its exponentials relative to it
     float m = -INFINITY;
+    if constexpr (W == 8) {
+      __nv_bfloat162 m2 = __floats2bfloat162_rn(-INFINITY, -INFINITY);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int v = j * THREADS + tid;
-      if (v < nvec) {
-        Vec16<T> r; r.load(zs + (size_t)v * W);
-        if constexpr (W == 8) {
+      for (int j = 0; j < NV; ++j) {
+        const int v = j * THREADS + tid;
+        if (v < nvec) {
+          Vec16<T> r; r.load(zs + (size_t)v * W);
           const __nv_bfloat162* h2 = reinterpret_cast<const __nv_bfloat162*>(&r.raw);
-          const __nv_bfloat162 m2 = __hmax2(__hmax2(h2[0], h2[1]), __hmax2(h2[2], h2[3]));
-          m = fmaxf(m, fmaxf(__low2float(m2), __high2float(m2)));
-        } else {
+          m2 = __hmax2(m2, __hmax2(__hmax2(h2[0], h2[1]), __hmax2(h2[2], h2[3])));
+        }
+      }
+      m = fmaxf(__low2float(m2), __high2float(m2));
+    } else {
+#pragma unroll
+      for (int j = 0; j < NV; ++j) {
+        const int v = j * THREADS + tid;
+        if (v < nvec) {
+          Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
           for (int i = 0; i < W; ++i) m = fmaxf(m, r.get(i));
         }
@@ -384,51 +430,56 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
     }
     const bool none = m == -INFINITY;
     const float mine = none ? 0.f : m;
-    float e[NV][W];
-    float sT = 0.f, s1 = 0.f;
-    const uint64_t one2 = tc::pack2(1.0f, 1.0f), cT2 = tc::pack2(p.cT, p.cT), neg2 = tc::pack2(-mine, -mine);
-    const uint64_t c12 = tc::pack2(p.c1, p.c1);
+    uint64_t e[NV][W / 2];
+    uint64_t sT2 = 0ull, s12 = 0ull;
+    const uint64_t neg2 = tc::pack2(-mine, -mine), cT2 = tc::pack2(p.cT, p.cT), c12 = tc::pack2(p.c1, p.c1);
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int v = j * THREADS + tid;
       if (v < nvec) {
         Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
-        for (int i = 0; i < W; i += 2) {
-          const uint64_t dd = tc::fma2(tc::pack2(r.get(i), r.get(i + 1)), one2, neg2);      // z - maximum
+        for (int i = 0; i < W / 2; ++i) {
+          const uint64_t dd = add2(pair_of(r, i), neg2);         // z - maximum
           float a, c;
           tc::unpack2(tc::mul2(dd, cT2), a, c);
-          e[j][i] = ex2(a); e[j][i + 1] = ex2(c);
-          sT += e[j][i]; sT += e[j][i + 1];
-          if constexpr (MODE == EXP_HALF) { s1 = fmaf(e[j][i], e[j][i], s1); s1 = fmaf(e[j][i + 1], e[j][i + 1], s1); }
+          e[j][i] = tc::pack2(ex2(a), ex2(c));
+          sT2 = add2(sT2, e[j][i]);
+          if constexpr (MODE == EXP_HALF) s12 = tc::fma2(e[j][i], e[j][i], s12);
           if constexpr (MODE == EXP_TWO) {
             tc::unpack2(tc::mul2(dd, c12), a, c);
-            s1 += ex2(a); s1 += ex2(c);
+            s12 = add2(s12, tc::pack2(ex2(a), ex2(c)));
           }
         }
       }
     }
+    float sT, s1;
+    {
+      float a, c;
+      tc::unpack2(sT2, a, c); sT = a + c;
+      tc::unpack2(s12, a, c); s1 = a + c;
+    }
     // ---- warp 0: the teacher's distribution
     float tsum = 0.f, tmax = -INFINITY;
     if (warp == 0) {
-      const bool left = head_left || tail_left;          // another thread's patch may not be visible yet: the logits themselves
+      const bool left = row == 0 || row == M - 1;        // another thread's patch may not be visible yet: the logits themselves
       for (int j = lane; j < k; j += 32) {
-        const int v = sh_idx[par][j];
+        const int v = sh_idx[slot][j];
         const bool ok = v >= 0 && v < V;
-        const float t = ok ? sh_q[par][j] : -INFINITY;
-        if (!ok) sh_idx[par][j] = -1;
-        sh_q[par][j] = t;
-        sh_z[par][j] = !ok ? 0.f : to_f<T>(left ? logits[row * p.ld + v] : zs[s + v]);
+        const float t = ok ? sh_q[slot][j] : -INFINITY;
+        if (!ok) sh_idx[slot][j] = -1;
+        sh_q[slot][j] = t;
+        sh_z[slot][j] = !ok ? 0.f : to_f<T>(left ? logits[row * p.ld + v] : zs[s + v]);
         tmax = t != t || tmax != tmax ? __uint_as_float(0x7fffffffu) : fmaxf(tmax, t);
       }
-      for (int j = k + lane; j < (k + 3) / 4 * 4; j += 32) sh_idx[par][j] = -1;
+      for (int j = k + lane; j < (k + 3) / 4 * 4; j += 32) sh_idx[slot][j] = -1;
       const bool nan = __any_sync(0xffffffffu, tmax != tmax);
       tmax = nan ? __uint_as_float(0x7fffffffu) : warp_max(tmax);
-      for (int j = lane; j < k; j += 32) tsum += expf((sh_q[par][j] - tmax) * inv_t);       // not used where tmax is -inf
+      for (int j = lane; j < k; j += 32) tsum += expf((sh_q[slot][j] - tmax) * p.inv_t);       // not used where tmax is -inf
       tsum = warp_sum(tsum);
       if (lane == 0) {
-        sh_zy[par] = p.labels ? to_f<T>(left ? logits[row * p.ld + y] : zs[s + y]) : 0.f;
-        sh_teach[par] = tmax != -INFINITY && p.wk != 0.f;    // else the teacher says nothing about this row
+        sh_zy[slot] = p.labels ? to_f<T>(left ? logits[row * p.ld + y] : zs[s + y]) : 0.f;
+        sh_teach[slot] = tmax != -INFINITY && p.wk != 0.f;     // else the teacher says nothing about this row
       }
     }
     // ---- the row's maximum and sums.  Without a maximum the sums are 0 or, from NaN, NaN: no factor
@@ -445,8 +496,10 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
       if constexpr (MODE != EXP_ONE) sh_s1[par][warp] = s1;
     }
     __syncthreads();
+    // the buffer whose logits nobody reads any more: this row's, or (EXP_TWO reads them again) the previous row's
+    if (tid == ISSUER && (MODE != EXP_TWO || (nbuf > 1 && done > 0))) issue_next();
+    if (done > 0 && warp >= 2) write_targets(slot == 0 ? SLOTS - 1 : slot - 1);
     ++done;
-    if (MODE != EXP_TWO && tid == 0) issue_next();       // the logits are not read again
     {
       const float rm = lane < NW ? sh_m[par][lane] : -INFINITY;
       m = warp_max(rm);
@@ -457,82 +510,76 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
       else s1 = sT;
     }
     const float base = m == -INFINITY ? 0.f : m;
-    const bool teach = sh_teach[par] != 0;
-    // ---- warp 0: the divergence and the row's loss
+    const bool teach = sh_teach[slot] != 0;
+    const float wkT = teach ? p.wk * p.temp : 0.f;
+    const float f1 = MODE == EXP_ONE ? (p.wc + wkT) / s1 * p.inv_n : p.wc / s1 * p.inv_n, fT = MODE == EXP_ONE ? 0.f : wkT / sT * p.inv_n;
+    // ---- warp 0: the divergence, the row's loss, and what its targets need
     if (warp == 0) {
       const float log_s1 = logf(s1), log_sT = logf(sT), log_ts = logf(tsum);
       float kl = 0.f;
       for (int j = lane; j < k; j += 32) {
-        const float lq = (sh_q[par][j] - tmax) * inv_t - log_ts;
+        const float lq = (sh_q[slot][j] - tmax) * p.inv_t - log_ts;
         const float q = teach ? expf(lq) : 0.f;
-        if (q != 0.f) kl += q * fmaf(p.temp, lq + log_sT, base - sh_z[par][j]);      // T times the divergence: (z - base) / T could overflow
-        sh_q[par][j] = q;
+        if (q != 0.f) kl += q * fmaf(p.temp, lq + log_sT, base - sh_z[slot][j]);      // T times the divergence: (z - base) / T could overflow
+        sh_q[slot][j] = q;
       }
       kl = warp_sum(kl);
       if (lane == 0) {
         float r = teach ? p.wk * p.temp * kl : 0.f;
-        if (p.wc != 0.f) r += p.wc * (log_s1 - (sh_zy[par] - base));
+        if (p.wc != 0.f) r += p.wc * (log_s1 - (sh_zy[slot] - base));
         p.rows[row] = r;
+        sh_f1[slot] = f1; sh_fT[slot] = fT; sh_base[slot] = base; sh_fq[slot] = wkT * p.inv_n;
+        sh_row[slot] = row; sh_y[slot] = p.labels ? y : -1;
       }
-      fetch_teacher(row + gridDim.x, par ^ 1);
+      fetch_teacher(row + gridDim.x, slot == SLOTS - 1 ? 0 : slot + 1);
     }
-    // ---- gradient
-    const float wkT = teach ? p.wk * p.temp : 0.f;
-    const float f1 = MODE == EXP_ONE ? (p.wc + wkT) / s1 * inv_n : p.wc / s1 * inv_n, fT = MODE == EXP_ONE ? 0.f : wkT / sT * inv_n;
-    // of this thread's exponentials, which are relative to its own maximum
+    // ---- gradient, from this thread's exponentials, which are relative to its own maximum
     const float up = none ? 1.f : ex2((mine - base) * p.cT);           // (a thread of -inf alone has exponentials of 0)
     const float g1 = MODE == EXP_ONE ? f1 * up : MODE == EXP_HALF ? f1 * (up * up) : f1, gT = fT * up;
+    const uint64_t g12 = tc::pack2(g1, g1), gT2 = tc::pack2(gT, gT), nb2 = tc::pack2(-base, -base);
+    if (warp == 1 && lane < 2 * W) {       // the ragged ends, one logit per lane
+      const int which = lane / W, i = lane % W, q = (which ? last * W : 0) + i;
+      if ((which ? ragged_last : ragged_first && !(last == 0 && ragged_last)) && q >= s && q < end) {
+        const float z = to_f<T>(sh_edge[par][which][i]) - base, x = ex2(z * p.cT);
+        out[q] = from_f<T>(MODE == EXP_ONE ? f1 * x : MODE == EXP_HALF ? x * fmaf(x, f1, fT) : fmaf(f1, ex2(z * p.c1), fT * x));
+      }
+    }
+    const int v_from = ragged_first ? 1 : 0, v_to = ragged_last ? last : nvec;
 #pragma unroll
     for (int j = 0; j < NV; ++j) {
       const int v = j * THREADS + tid;
-      if (v < nvec) {
-        float o[W];
+      if (v >= v_from && v < v_to) {
+        Vec16<T> o;
+        Vec16<T> r;
+        if constexpr (MODE == EXP_TWO) r.load(zs + (size_t)v * W);
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-          if constexpr (MODE == EXP_ONE) o[i] = e[j][i] * g1;
-          if constexpr (MODE == EXP_HALF) o[i] = e[j][i] * fmaf(e[j][i], g1, gT);
+        for (int i = 0; i < W / 2; ++i) {
+          uint64_t w;
+          if constexpr (MODE == EXP_ONE) w = tc::mul2(e[j][i], g12);
+          if constexpr (MODE == EXP_HALF) w = tc::mul2(e[j][i], tc::fma2(e[j][i], g12, gT2));
+          float a, c;
+          if constexpr (MODE == EXP_TWO) {
+            tc::unpack2(tc::mul2(add2(pair_of(r, i), nb2), c12), a, c);
+            w = tc::fma2(e[j][i], gT2, tc::mul2(g12, tc::pack2(ex2(a), ex2(c))));
+          }
+          tc::unpack2(w, a, c);
+          if constexpr (W == 8) reinterpret_cast<__nv_bfloat162*>(&o.raw)[i] = __floats2bfloat162_rn(a, c);
+          else { o.set(2 * i, a); o.set(2 * i + 1, c); }
         }
-        if constexpr (MODE == EXP_TWO) {
-          Vec16<T> r; r.load(zs + (size_t)v * W);
-#pragma unroll
-          for (int i = 0; i < W; ++i) o[i] = fmaf(e[j][i], gT, g1 * ex2((r.get(i) - base) * p.c1));
-        }
-        if (p.same && v * W >= s && (v + 1) * W <= end) {
-          store_vec<T>(out + (int64_t)v * W, o);
-        } else {
-#pragma unroll
-          for (int i = 0; i < W; ++i)
-            if (v * W + i >= s && v * W + i < end) out[v * W + i] = from_f<T>(o[i]);
-        }
+        if (p.same) o.store(out + (int64_t)v * W);
+        else store_each(out + (int64_t)v * W, o);
       }
     }
     if (out_end > end) zeros(end, out_end);
-    __syncthreads();
-    if (MODE == EXP_TWO && tid == 0) issue_next();
-    // ---- the entries with a target, from the last threads on: the first entry of an index writes for all of them
-    auto value = [&](float z) {
-      if constexpr (MODE == EXP_TWO) return fmaf(f1, ex2((z - base) * p.c1), fT * ex2((z - base) * p.cT));
-      const float x = ex2((z - base) * p.cT);
-      return MODE == EXP_ONE ? f1 * x : x * fmaf(x, f1, fT);
-    };
-    for (int j = THREADS - 1 - tid; j <= k; j += THREADS) {
-      const int v = j < k ? sh_idx[par][j] : p.labels ? y : -1;        // entry k: the label
-      if (v < 0) continue;
-      bool first = true;
-      float q = 0.f;
-      for (int i = 0; i < k; i += 4) {
-        const int4 w = *reinterpret_cast<const int4*>(&sh_idx[par][i]);
-        if (w.x == v) { if (i < j) first = false; q += sh_q[par][i]; }
-        if (w.y == v) { if (i + 1 < j) first = false; q += sh_q[par][i + 1]; }
-        if (w.z == v) { if (i + 2 < j) first = false; q += sh_q[par][i + 2]; }
-        if (w.w == v) { if (i + 3 < j) first = false; q += sh_q[par][i + 3]; }
-      }
-      if (!first) continue;
-      float r = value(j < k ? sh_z[par][j] : sh_zy[par]) - wkT * inv_n * q;
-      if (p.labels && v == y) r -= p.wc * inv_n;
-      out[s + v] = from_f<T>(r);
+    if (MODE == EXP_TWO && nbuf == 1) {
+      __syncthreads();
+      if (tid == ISSUER) issue_next();
     }
-    par ^= 1;
+    slot = slot == SLOTS - 1 ? 0 : slot + 1;
+  }
+  if (done > 0) {
+    __syncthreads();
+    if (warp >= 2) write_targets(slot == 0 ? SLOTS - 1 : slot - 1);
   }
 }
 
@@ -572,7 +619,7 @@ namespace {
 // Rows up to this many labels are counted by every block of the ring kernel instead of a launch in front of it.
 constexpr int COUNT_HERE = 4096;
 constexpr int RING_MAX_VOCAB = 53248 - 7;              // the widest block: 512 threads x 104 logits, at any alignment
-constexpr int RING_TABLES = 8192, RING_BYTES = 232448 - 1024 - RING_TABLES;     // static tables; dynamic shared memory of all blocks of an SM
+constexpr int RING_TABLES = 11264, RING_BYTES = 232448 - 1024 - RING_TABLES;     // static tables; dynamic shared memory of all blocks of an SM
 
 template <typename T, int E, int THREADS, int MINB, int MODE>
 cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, int* status, cudaStream_t st) {
@@ -607,7 +654,7 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
                     float temperature, float wc, float wk, int normalizer, void* grad, int64_t ldo, float* rows, int* n_valid, float* loss,
                     int* status, cudaStream_t st) {
   DistillArgs p;
-  p.labels = labels; p.idx = idx; p.t = t; p.ld = ld; p.ldo = ldo; p.V = V; p.k = k; p.temp = temperature; p.wc = wc; p.wk = wk; p.rows = rows;
+  p.labels = labels; p.idx = idx; p.t = t; p.ld = ld; p.ldo = ldo; p.V = V; p.k = k; p.temp = temperature; p.inv_t = 1.0f / temperature; p.inv_n = 0.f; p.wc = wc; p.wk = wk; p.rows = rows;
   const bool count = labels != nullptr && normalizer <= 0;
   p.n_valid = count ? n_valid : nullptr;
   p.n_fixed = normalizer > 0 ? normalizer : M;
