@@ -41,12 +41,6 @@ struct DistillArgs {
   int count_here;          // the ring kernel counts the labels and leaves the count in n_valid
 };
 
-// one by one, where the gradient's rows start at another place of a 16-byte vector (out of line: the loop around it is unrolled)
-template <typename T> __device__ __noinline__ void store_each(T* p, Vec16<T> o) {
-#pragma unroll
-  for (int i = 0; i < Vec16<T>::N; ++i) p[i] = reinterpret_cast<const T*>(&o.raw)[i];
-}
-
 // Running maximum and sums of exponentials relative to it.
 struct Online { float m, s1, sT; };
 template <int MODE> __device__ __forceinline__ void online_merge(Online& a, const Online& b, float c1, float cT) {
@@ -262,14 +256,20 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
 __device__ __forceinline__ uint64_t pair_of(const Vec16<bf16>& r, int i) { return tc::bf16x2_to_f32x2(reinterpret_cast<const uint32_t*>(&r.raw)[i]); }
 __device__ __forceinline__ uint64_t pair_of(const Vec16<float>& r, int i) { return tc::pack2(r.get(2 * i), r.get(2 * i + 1)); }
 
+__device__ __forceinline__ uint64_t exp_pair(uint64_t x) {
+  float a, c;
+  tc::unpack2(x, a, c);
+  return tc::pack2(ex2(a), ex2(c));
+}
+
 constexpr int SLOTS = 3;   // rows whose tables are in use at once: the next one's, this one's, the one whose targets are being written
 
-// E: logits per thread; MINB: blocks per SM.  One barrier per row: behind it every logit of the row has been read, every sum is
+// MINB: blocks per SM.  One barrier per row (two with one buffer): behind it every logit of the row has been read, every sum is
 // there, and the previous row's gradient has been written but for the entries with a target, which follow then.
-template <typename T, int E, int THREADS, int MINB, int MODE>
+template <typename T, int THREADS, int MINB, int MODE>
 __global__ void __launch_bounds__(THREADS, MINB)
 distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p, int M, int nbuf, int buf_bytes, int* status) {
-  constexpr int W = Vec16<T>::N, NV = E / W, NW = THREADS / 32, ISSUER = THREADS - 32;
+  constexpr int W = Vec16<T>::N, NW = THREADS / 32, ISSUER = THREADS - 32;
   extern __shared__ __align__(128) uint8_t smem[];       // nbuf rows
   __shared__ __align__(16) int sh_idx[SLOTS][DISTILL_MAX_K];
   __shared__ float sh_q[SLOTS][DISTILL_MAX_K], sh_z[SLOTS][DISTILL_MAX_K];
@@ -407,49 +407,36 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
     float m = -INFINITY;
     if constexpr (W == 8) {
       __nv_bfloat162 m2 = __floats2bfloat162_rn(-INFINITY, -INFINITY);
-#pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int v = j * THREADS + tid;
-        if (v < nvec) {
-          Vec16<T> r; r.load(zs + (size_t)v * W);
-          const __nv_bfloat162* h2 = reinterpret_cast<const __nv_bfloat162*>(&r.raw);
-          m2 = __hmax2(m2, __hmax2(__hmax2(h2[0], h2[1]), __hmax2(h2[2], h2[3])));
-        }
+#pragma unroll 4
+      for (int v = tid; v < nvec; v += THREADS) {
+        Vec16<T> r; r.load(zs + (size_t)v * W);
+        const __nv_bfloat162* h2 = reinterpret_cast<const __nv_bfloat162*>(&r.raw);
+        m2 = __hmax2(m2, __hmax2(__hmax2(h2[0], h2[1]), __hmax2(h2[2], h2[3])));
       }
       m = fmaxf(__low2float(m2), __high2float(m2));
     } else {
+#pragma unroll 4
+      for (int v = tid; v < nvec; v += THREADS) {
+        Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
-      for (int j = 0; j < NV; ++j) {
-        const int v = j * THREADS + tid;
-        if (v < nvec) {
-          Vec16<T> r; r.load(zs + (size_t)v * W);
-#pragma unroll
-          for (int i = 0; i < W; ++i) m = fmaxf(m, r.get(i));
-        }
+        for (int i = 0; i < W; ++i) m = fmaxf(m, r.get(i));
       }
     }
-    const bool none = m == -INFINITY;
-    const float mine = none ? 0.f : m;
-    uint64_t e[NV][W / 2];
+    const float mine = m == -INFINITY ? 0.f : m;
     uint64_t sT2 = 0ull, s12 = 0ull;
-    const uint64_t neg2 = tc::pack2(-mine, -mine), cT2 = tc::pack2(p.cT, p.cT), c12 = tc::pack2(p.c1, p.c1);
-#pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int v = j * THREADS + tid;
-      if (v < nvec) {
+    const uint64_t cT2 = tc::pack2(p.cT, p.cT), c12 = tc::pack2(p.c1, p.c1);
+    {
+      const uint64_t neg2 = tc::pack2(-mine, -mine);
+#pragma unroll 2
+      for (int v = tid; v < nvec; v += THREADS) {
         Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
         for (int i = 0; i < W / 2; ++i) {
           const uint64_t dd = add2(pair_of(r, i), neg2);         // z - maximum
-          float a, c;
-          tc::unpack2(tc::mul2(dd, cT2), a, c);
-          e[j][i] = tc::pack2(ex2(a), ex2(c));
-          sT2 = add2(sT2, e[j][i]);
-          if constexpr (MODE == EXP_HALF) s12 = tc::fma2(e[j][i], e[j][i], s12);
-          if constexpr (MODE == EXP_TWO) {
-            tc::unpack2(tc::mul2(dd, c12), a, c);
-            s12 = add2(s12, tc::pack2(ex2(a), ex2(c)));
-          }
+          const uint64_t e = exp_pair(tc::mul2(dd, cT2));
+          sT2 = add2(sT2, e);
+          if constexpr (MODE == EXP_HALF) s12 = tc::fma2(e, e, s12);
+          if constexpr (MODE == EXP_TWO) s12 = add2(s12, exp_pair(tc::mul2(dd, c12)));
         }
       }
     }
@@ -496,8 +483,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
       if constexpr (MODE != EXP_ONE) sh_s1[par][warp] = s1;
     }
     __syncthreads();
-    // the buffer whose logits nobody reads any more: this row's, or (EXP_TWO reads them again) the previous row's
-    if (tid == ISSUER && (MODE != EXP_TWO || (nbuf > 1 && done > 0))) issue_next();
+    if (tid == ISSUER && nbuf > 1 && done > 0) issue_next();           // nobody reads the previous row's logits any more
     if (done > 0 && warp >= 2) write_targets(slot == 0 ? SLOTS - 1 : slot - 1);
     ++done;
     {
@@ -533,10 +519,8 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
       }
       fetch_teacher(row + gridDim.x, slot == SLOTS - 1 ? 0 : slot + 1);
     }
-    // ---- gradient, from this thread's exponentials, which are relative to its own maximum
-    const float up = none ? 1.f : ex2((mine - base) * p.cT);           // (a thread of -inf alone has exponentials of 0)
-    const float g1 = MODE == EXP_ONE ? f1 * up : MODE == EXP_HALF ? f1 * (up * up) : f1, gT = fT * up;
-    const uint64_t g12 = tc::pack2(g1, g1), gT2 = tc::pack2(gT, gT), nb2 = tc::pack2(-base, -base);
+    // ---- gradient
+    const uint64_t f12 = tc::pack2(f1, f1), fT2 = tc::pack2(fT, fT), neg2 = tc::pack2(-base, -base);
     if (warp == 1 && lane < 2 * W) {       // the ragged ends, one logit per lane
       const int which = lane / W, i = lane % W, q = (which ? last * W : 0) + i;
       if ((which ? ragged_last : ragged_first && !(last == 0 && ragged_last)) && q >= s && q < end) {
@@ -544,34 +528,31 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
         out[q] = from_f<T>(MODE == EXP_ONE ? f1 * x : MODE == EXP_HALF ? x * fmaf(x, f1, fT) : fmaf(f1, ex2(z * p.c1), fT * x));
       }
     }
-    const int v_from = ragged_first ? 1 : 0, v_to = ragged_last ? last : nvec;
+    const int v_to = ragged_last ? last : nvec;
+#pragma unroll 2
+    for (int v = tid == 0 && ragged_first ? THREADS : tid; v < v_to; v += THREADS) {
+      Vec16<T> r, o;
+      r.load(zs + (size_t)v * W);
 #pragma unroll
-    for (int j = 0; j < NV; ++j) {
-      const int v = j * THREADS + tid;
-      if (v >= v_from && v < v_to) {
-        Vec16<T> o;
-        Vec16<T> r;
-        if constexpr (MODE == EXP_TWO) r.load(zs + (size_t)v * W);
-#pragma unroll
-        for (int i = 0; i < W / 2; ++i) {
-          uint64_t w;
-          if constexpr (MODE == EXP_ONE) w = tc::mul2(e[j][i], g12);
-          if constexpr (MODE == EXP_HALF) w = tc::mul2(e[j][i], tc::fma2(e[j][i], g12, gT2));
-          float a, c;
-          if constexpr (MODE == EXP_TWO) {
-            tc::unpack2(tc::mul2(add2(pair_of(r, i), nb2), c12), a, c);
-            w = tc::fma2(e[j][i], gT2, tc::mul2(g12, tc::pack2(ex2(a), ex2(c))));
-          }
-          tc::unpack2(w, a, c);
-          if constexpr (W == 8) reinterpret_cast<__nv_bfloat162*>(&o.raw)[i] = __floats2bfloat162_rn(a, c);
-          else { o.set(2 * i, a); o.set(2 * i + 1, c); }
-        }
-        if (p.same) o.store(out + (int64_t)v * W);
-        else store_each(out + (int64_t)v * W, o);
+      for (int i = 0; i < W / 2; ++i) {
+        const uint64_t dd = add2(pair_of(r, i), neg2);
+        const uint64_t e = exp_pair(tc::mul2(dd, cT2));
+        uint64_t w;
+        if constexpr (MODE == EXP_ONE) w = tc::mul2(e, f12);
+        if constexpr (MODE == EXP_HALF) w = tc::mul2(e, tc::fma2(e, f12, fT2));
+        if constexpr (MODE == EXP_TWO) w = tc::fma2(e, fT2, tc::mul2(f12, exp_pair(tc::mul2(dd, c12))));
+        float a, c;
+        tc::unpack2(w, a, c);
+        if constexpr (W == 8) reinterpret_cast<__nv_bfloat162*>(&o.raw)[i] = __floats2bfloat162_rn(a, c);
+        else { o.set(2 * i, a); o.set(2 * i + 1, c); }
       }
+      if (p.same) o.store(out + (int64_t)v * W);
+      else
+#pragma unroll
+        for (int i = 0; i < W; ++i) out[v * W + i] = reinterpret_cast<const T*>(&o.raw)[i];
     }
     if (out_end > end) zeros(end, out_end);
-    if (MODE == EXP_TWO && nbuf == 1) {
+    if (nbuf == 1) {
       __syncthreads();
       if (tid == ISSUER) issue_next();
     }
@@ -618,12 +599,12 @@ namespace {
 
 // Rows up to this many labels are counted by every block of the ring kernel instead of a launch in front of it.
 constexpr int COUNT_HERE = 4096;
-constexpr int RING_MAX_VOCAB = 53248 - 7;              // the widest block: 512 threads x 104 logits, at any alignment
 constexpr int RING_TABLES = 11264, RING_BYTES = 232448 - 1024 - RING_TABLES;     // static tables; dynamic shared memory of all blocks of an SM
 
-template <typename T, int E, int THREADS, int MINB, int MODE>
-cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, int* status, cudaStream_t st) {
-  const auto kernel = distill_ring_kernel<T, E, THREADS, MINB, MODE>;
+template <typename T, int THREADS, int MODE>
+cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, int buf, int nbuf, int fit, int* status, cudaStream_t st) {
+  constexpr int MINB = 1024 / THREADS;
+  const auto kernel = distill_ring_kernel<T, THREADS, MINB, MODE>;
   static PerDeviceOnce once;
   const int dev = current_device();
   if (once.needed(dev)) {
@@ -631,21 +612,21 @@ cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, i
     if (e != cudaSuccess) return e;
     once.done(dev);
   }
-  const int buf = (int)(((size_t)p.V * sizeof(T) + 15) / 16 * 16 + 16), nbuf = 2 * buf <= RING_BYTES ? 2 : 1;
-  const int fit = (RING_BYTES + RING_TABLES) / (nbuf * buf + RING_TABLES), per_sm = fit < MINB ? fit : MINB;
-  const int64_t most = (int64_t)num_sms() * per_sm;
+  const int64_t most = (int64_t)num_sms() * (fit < MINB ? fit : MINB);
   return launch_overlapped(kernel, dim3((unsigned)(M < most ? M : most)), dim3(THREADS), (size_t)nbuf * buf, st, logits, grad, p, M, nbuf, buf, status);
 }
 
-// The smallest block whose registers hold a row.
+// As many rows per SM as shared memory holds, up to eight, and 1024 threads for all of them; two buffers per row where eight
+// rows have room for them.
 template <typename T, int MODE>
 cudaError_t ring(const T* logits, T* grad, const DistillArgs& p, int M, int* status, cudaStream_t st) {
-  const int need = p.V + Vec16<T>::N - 1;              // at any alignment
-  if (need <= 2048) return launch_ring<T, 16, 128, 8, MODE>(logits, grad, p, M, status, st);
-  if (need <= 8192) return launch_ring<T, 64, 128, 4, MODE>(logits, grad, p, M, status, st);
-  if (need <= 16384) return launch_ring<T, 64, 256, 2, MODE>(logits, grad, p, M, status, st);
-  if (need <= 32768) return launch_ring<T, 64, 512, 1, MODE>(logits, grad, p, M, status, st);
-  return launch_ring<T, 104, 512, 1, MODE>(logits, grad, p, M, status, st);
+  const int buf = (int)(((size_t)p.V * sizeof(T) + 15) / 16 * 16 + 16);
+  const int one = (RING_BYTES + RING_TABLES) / (buf + RING_TABLES), two = (RING_BYTES + RING_TABLES) / (2 * buf + RING_TABLES);
+  if (two >= 8) return launch_ring<T, 128, MODE>(logits, grad, p, M, buf, 2, two, status, st);
+  if (one >= 6) return launch_ring<T, 128, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  if (one >= 3) return launch_ring<T, 256, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  if (one == 2) return launch_ring<T, 512, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  return launch_ring<T, 1024, MODE>(logits, grad, p, M, buf, 1, one, status, st);
 }
 
 }  // namespace
@@ -666,7 +647,7 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
   cudaError_t e = cudaSuccess;
   const size_t es = dtype_size(dt);
   p.same = ((reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(grad)) & 15u) == 0 && ((ld - ldo) * (int64_t)es) % 16 == 0;
-  const bool in_ring = V <= RING_MAX_VOCAB;
+  const bool in_ring = (int64_t)V * es + 32 <= RING_BYTES;
   p.count_here = in_ring && count && M <= COUNT_HERE;
   if (count && !p.count_here) {
     e = launch_overlapped(distill_count_kernel, dim3(1), dim3(1024), 0, st, labels, M, V, n_valid);
