@@ -35,7 +35,7 @@ struct DistillArgs {
   int V, k;
   float temp, wc, wk;
   float c1, cT;            // log2(e) / temperature of the first and second exponential
-  float inv_t, inv_n;      // inv_n: set by the kernel
+  float inv_t;
   float* rows; int* n_valid; int n_fixed;
   int same;                // rows of logits and gradient start at the same place of a 16-byte vector
   int count_here;          // the ring kernel counts the labels and leaves the count in n_valid
@@ -262,22 +262,30 @@ __device__ __forceinline__ uint64_t exp_pair(uint64_t x) {
   return tc::pack2(ex2(a), ex2(c));
 }
 
-constexpr int SLOTS = 3;   // rows whose tables are in use at once: the next one's, this one's, the one whose targets are being written
+// maximum over a warp in one instruction, on integers in the order of the floats (no NaN comes here)
+__device__ __forceinline__ float warp_max_redux(float v) {
+  const int i = __float_as_int(v), o = i ^ ((i >> 31) & 0x7fffffff), m = __reduce_max_sync(0xffffffffu, o);
+  return __int_as_float(m ^ ((m >> 31) & 0x7fffffff));
+}
 
-// MINB: blocks per SM.  One barrier per row (two with one buffer): behind it every logit of the row has been read, every sum is
-// there, and the previous row's gradient has been written but for the entries with a target, which follow then.
+constexpr int SLOTS = 4;     // rows whose tables are in use at once: two ahead, this one, the one whose targets are being written
+constexpr int BATCH = 128;   // rows of a block that are looked at together for those that take part
+
+// MINB: blocks per SM.  One barrier per row (two with one buffer).  Behind it every sum is there, and the previous row's gradient
+// has been written but for the entries with a target, which follow then.  What a row needs besides its logits is spread over the
+// warps: 0 the row's loss, 1 the ragged ends and the teacher's distribution of the next row, the others the previous row's targets.
 template <typename T, int THREADS, int MINB, int MODE>
 __global__ void __launch_bounds__(THREADS, MINB)
 distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p, int M, int nbuf, int buf_bytes, int* status) {
   constexpr int W = Vec16<T>::N, NW = THREADS / 32, ISSUER = THREADS - 32;
   extern __shared__ __align__(128) uint8_t smem[];       // nbuf rows
   __shared__ __align__(16) int sh_idx[SLOTS][DISTILL_MAX_K];
-  __shared__ float sh_q[SLOTS][DISTILL_MAX_K], sh_z[SLOTS][DISTILL_MAX_K];
-  __shared__ float sh_m[2][32], sh_sT[2][32], sh_s1[2][32];
+  __shared__ float sh_q[SLOTS][DISTILL_MAX_K], sh_z[2][DISTILL_MAX_K];
+  __shared__ float sh_m[2][NW], sh_sT[2][NW], sh_s1[2][NW];
   __shared__ T sh_edge[2][2][W];                         // logits of the row's ragged first and last vector
-  __shared__ float sh_zy[SLOTS], sh_f1[SLOTS], sh_fT[SLOTS], sh_base[SLOTS], sh_fq[SLOTS];
-  __shared__ int64_t sh_row[SLOTS];
-  __shared__ int sh_y[SLOTS], sh_teach[SLOTS], sh_count[32], sh_abort;
+  __shared__ float sh_zy[2], sh_f1[2], sh_fT[2], sh_base[2], sh_fq[2];
+  __shared__ float sh_tmax[SLOTS], sh_lts[SLOTS];        // log q_j = (t_j - tmax) / T - lts
+  __shared__ int sh_teach[SLOTS], sh_rows[BATCH], sh_ys[BATCH], sh_cnt[NW], sh_abort;
   __shared__ __align__(8) uint64_t bars[2];
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const int V = p.V, k = p.k;
@@ -292,40 +300,65 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
   __syncthreads();
   overlap_sync();
 
-  auto label_of = [&](int64_t r) { return p.labels && r < M ? p.labels[r] : 0; };
   auto takes_part = [&](int y) { return y >= 0 && y < V; };
-  // thread ISSUER: the next row that takes part into the next buffer
-  int64_t ahead = blockIdx.x;
-  int issued = 0;
-  auto issue_next = [&]() {
-    while (ahead < M && !takes_part(label_of(ahead))) ahead += gridDim.x;
-    if (ahead >= M) return;
-    const int b = issued % nbuf;
-    const uintptr_t a0 = reinterpret_cast<uintptr_t>(logits + ahead * p.ld), a1 = a0 + (uintptr_t)V * sizeof(T), f0 = a0 & ~(uintptr_t)15;
-    const uintptr_t lo = ahead == 0 && f0 < a0 ? f0 + 16 : f0, hi = ahead == M - 1 ? a1 & ~(uintptr_t)15 : (a1 + 15) & ~(uintptr_t)15;
+  int n = p.n_fixed;
+  if (p.n_valid && !p.count_here) n = *p.n_valid;
+  if (p.count_here) {                      // few labels: every block counts them itself
+    int c = 0;
+    for (int i = tid; i < M; i += THREADS) c += takes_part(p.labels[i]) ? 1 : 0;
+    c = __reduce_add_sync(0xffffffffu, c);
+    if (lane == 0) sh_cnt[warp] = c;
+    __syncthreads();
+    n = 0;
+    for (int w = 0; w < NW; ++w) n += sh_cnt[w];
+    if (blockIdx.x == 0 && tid == 0) *p.n_valid = n;
+  }
+  const float inv_n = 1.0f / (float)(n > 0 ? n : 1);
+
+  // thread ISSUER: logits of a row into a buffer
+  auto issue = [&](int row, int b) {
+    const uintptr_t a0 = reinterpret_cast<uintptr_t>(logits + row * p.ld), a1 = a0 + (uintptr_t)V * sizeof(T), f0 = a0 & ~(uintptr_t)15;
+    const uintptr_t lo = row == 0 && f0 < a0 ? f0 + 16 : f0, hi = row == M - 1 ? a1 & ~(uintptr_t)15 : (a1 + 15) & ~(uintptr_t)15;
     const uint32_t bytes = hi > lo ? (uint32_t)(hi - lo) : 0u, bar = tc::smem_u32(&bars[b]);
     tc::mbar_expect_tx(bar, bytes);
     if (bytes)
       asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
                    ::"r"(smem_base + (uint32_t)(b * buf_bytes) + (uint32_t)(lo - f0)), "l"(lo), "r"(bytes), "r"(bar) : "memory");
-    ++issued;
-    ahead += gridDim.x;
   };
-  // warp 0: a row's teacher entries into the tables, one row ahead; lane j % 32 copies entry j and reads it
-  auto fetch_teacher = [&](int64_t r, int slot) {
-    if (r < M)
-      for (int j = lane; j < k; j += 32) {
-        cp_async4(tc::smem_u32(&sh_idx[slot][j]), p.idx + r * k + j);
-        cp_async4(tc::smem_u32(&sh_q[slot][j]), p.t + r * k + j);
-      }
+  // warp 1: a row's teacher entries into the tables; lane j % 32 copies entry j and is the one that reads it
+  auto fetch_teacher = [&](int row, int slot) {
+    for (int j = lane; j < k; j += 32) {
+      cp_async4(tc::smem_u32(&sh_idx[slot][j]), p.idx + (int64_t)row * k + j);
+      cp_async4(tc::smem_u32(&sh_q[slot][j]), p.t + (int64_t)row * k + j);
+    }
   };
-  // from warp 2 on: the entries of the row in `slot` that carry a target; the first entry of an index writes for all of them
-  auto write_targets = [&](int slot) {
-    const float f1 = sh_f1[slot], fT = sh_fT[slot], base = sh_base[slot];
-    const int y = sh_y[slot];
-    T* out = grad + sh_row[slot] * p.ldo;
+  // warp 1: t -> q = softmax(t / T) over the row's entries, absent ones as index -1
+  auto teacher = [&](int slot) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    float tmax = -INFINITY, tsum = 0.f;
+    for (int j = lane; j < k; j += 32) {
+      const int v = sh_idx[slot][j];
+      const bool ok = v >= 0 && v < V;
+      const float t = ok ? sh_q[slot][j] : -INFINITY;
+      if (!ok) { sh_idx[slot][j] = -1; sh_q[slot][j] = t; }
+      tmax = t != t || tmax != tmax ? __uint_as_float(0x7fffffffu) : fmaxf(tmax, t);
+    }
+    for (int j = k + lane; j < (k + 3) / 4 * 4; j += 32) sh_idx[slot][j] = -1;
+    const bool nan = __any_sync(0xffffffffu, tmax != tmax);
+    tmax = warp_max_redux(nan ? 0.f : tmax);
+    if (nan) tmax = __uint_as_float(0x7fffffffu);
+    const bool teach = tmax != -INFINITY && p.wk != 0.f;     // else the teacher says nothing about this row
+    for (int j = lane; j < k; j += 32) tsum += teach ? expf((sh_q[slot][j] - tmax) * p.inv_t) : 0.f;
+    tsum = warp_sum(tsum);
+    for (int j = lane; j < k; j += 32) sh_q[slot][j] = teach ? expf((sh_q[slot][j] - tmax) * p.inv_t) / tsum : 0.f;
+    if (lane == 0) { sh_teach[slot] = teach; sh_tmax[slot] = tmax; sh_lts[slot] = logf(tsum); }
+  };
+  // from warp 2 on: the entries of a row that carry a target; the first entry of an index writes for all of them
+  auto write_targets = [&](int row, int y, int slot, int par) {
+    const float f1 = sh_f1[par], fT = sh_fT[par], base = sh_base[par];
+    T* out = grad + row * p.ldo;
     for (int j = tid - 64; j <= k; j += THREADS - 64) {
-      const int v = j < k ? sh_idx[slot][j] : y;         // entry k: the label (-1: no labels)
+      const int v = j < k ? sh_idx[slot][j] : p.labels ? y : -1;       // entry k: the label
       if (v < 0) continue;
       bool first = true;
       float q = 0.f;
@@ -337,230 +370,223 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
         if (w.w == v) { if (i + 3 < j) first = false; q += sh_q[slot][i + 3]; }
       }
       if (!first) continue;
-      const float z = (j < k ? sh_z[slot][j] : sh_zy[slot]) - base, x = ex2(z * p.cT);
+      const float z = (j < k ? sh_z[par][j] : sh_zy[par]) - base, x = ex2(z * p.cT);
       float r = MODE == EXP_ONE ? f1 * x : MODE == EXP_HALF ? x * fmaf(x, f1, fT) : fmaf(f1, ex2(z * p.c1), fT * x);
-      r -= sh_fq[slot] * q;
-      if (v == y) r -= p.wc * p.inv_n;
+      r -= sh_fq[par] * q;
+      if (p.labels && v == y) r -= p.wc * inv_n;
       out[v] = from_f<T>(r);
     }
   };
-  if (tid == ISSUER)
-    for (int b = 0; b < nbuf; ++b) issue_next();
-  if (warp == 0) fetch_teacher(blockIdx.x, 0);
-  int n = p.n_fixed;
-  if (p.n_valid && !p.count_here) n = *p.n_valid;
-  if (p.count_here) {                      // few labels: every block counts them itself
-    int c = 0;
-    for (int i = tid; i < M; i += THREADS) c += takes_part(p.labels[i]) ? 1 : 0;
-    c = __reduce_add_sync(0xffffffffu, c);
-    if (lane == 0) sh_count[warp] = c;
-    __syncthreads();
-    n = 0;
-    for (int w = 0; w < NW; ++w) n += sh_count[w];
-    if (blockIdx.x == 0 && tid == 0) *p.n_valid = n;
-  }
-  p.inv_n = 1.0f / (float)(n > 0 ? n : 1);
+  // all threads: positions [from, to) of a row of the gradient (position 0: a 16-byte boundary of the logits) become zero
+  auto zeros = [&](T* out, int from, int to) {
+    for (int v = from / W + tid; v * W < to; v += THREADS) {
+      if (p.same && v * W >= from && (v + 1) * W <= to) *reinterpret_cast<uint4*>(out + (int64_t)v * W) = make_uint4(0u, 0u, 0u, 0u);
+      else
+        for (int i = 0; i < W; ++i)
+          if (v * W + i >= from && v * W + i < to) out[v * W + i] = from_f<T>(0.f);
+    }
+  };
+  auto shift_of = [&](int row) { return (int)((reinterpret_cast<uintptr_t>(logits + row * p.ld) & 15u) / sizeof(T)); };
 
-  int done = 0, slot = 0;                  // rows that took part; tables of this row
-  int y_next = label_of(blockIdx.x);
-  for (int64_t row = blockIdx.x; row < M; row += gridDim.x) {
-    const int y = y_next;
-    y_next = label_of(row + gridDim.x);
-    const int s = (int)((reinterpret_cast<uintptr_t>(logits + row * p.ld) & 15u) / sizeof(T));
-    T* out = grad + row * p.ldo - s;       // position q = s + column
-    const int end = s + V, out_end = s + (int)p.ldo, nvec = (end + W - 1) / W, last = nvec - 1;
-    // positions [from, to) of the gradient become zero
-    auto zeros = [&](int from, int to) {
-      for (int v = from / W + tid; v * W < to; v += THREADS) {
-        if (p.same && v * W >= from && (v + 1) * W <= to) *reinterpret_cast<uint4*>(out + (int64_t)v * W) = make_uint4(0u, 0u, 0u, 0u);
-        else
-          for (int i = 0; i < W; ++i)
-            if (v * W + i >= from && v * W + i < to) out[v * W + i] = from_f<T>(0.f);
+  const uint64_t cT2 = tc::pack2(p.cT, p.cT), c12 = tc::pack2(p.c1, p.c1);
+  int used = 0;                            // rows copied so far: buffer used % nbuf, phase used / nbuf
+  for (int64_t row0 = blockIdx.x; row0 < M; row0 += (int64_t)BATCH * gridDim.x) {
+    // ---- which of the next rows take part
+    __syncthreads();                       // the previous batch's lists and tables
+    int count = 0;
+    for (int i0 = 0; i0 < BATCH; i0 += 32) {             // (every warp for itself; warp 0 writes the list)
+      const int64_t r = row0 + (int64_t)(i0 + lane) * gridDim.x;
+      const int y = r < M && p.labels ? p.labels[r] : 0;
+      const bool in = r < M && takes_part(y);
+      const uint32_t mask = __ballot_sync(0xffffffffu, in);
+      if (warp == 0 && in) {
+        const int at = count + __popc(mask & ((1u << lane) - 1u));
+        sh_rows[at] = (int)r;
+        sh_ys[at] = y;
       }
-    };
-    if (warp == 0) asm volatile("cp.async.wait_all;" ::: "memory");
-    if (!takes_part(y)) {
-      if (tid == 0) p.rows[row] = 0.f;
-      zeros(s, out_end);
-      if (warp == 0) fetch_teacher(row + gridDim.x, slot);     // over this row's entries: the other tables may still be read
-      continue;
+      uint32_t out_mask = __ballot_sync(0xffffffffu, r < M && !in);
+      while (out_mask) {                   // a row that takes no part: zeros
+        const int l = __ffs(out_mask) - 1;
+        out_mask &= out_mask - 1;
+        const int row = (int)(row0 + (int64_t)(i0 + l) * gridDim.x), s = shift_of(row);
+        if (tid == 0) p.rows[row] = 0.f;
+        zeros(grad + row * p.ldo - s, s, s + (int)p.ldo);
+      }
+      count += __popc(mask);
     }
-    const int b = done % nbuf, par = done & 1;
-    tc::mbar_wait(tc::smem_u32(&bars[b]), (uint32_t)(done / nbuf) & 1u, &sh_abort, status, 81);
-    T* zs = reinterpret_cast<T*>(smem + (size_t)b * buf_bytes);
-    // A ragged first or last vector (in the first and last row of all the copies left it out): the thread that owns it keeps its
-    // logits for the gradient and puts -inf around them.
-    const bool ragged_first = s > 0 || (last == 0 && end % W != 0), ragged_last = end % W != 0;
-    if ((tid == 0 && ragged_first) || (tid == last % THREADS && ragged_last)) {
-      const T* z = logits + row * p.ld - s;
-      const bool left = row == 0 || row == M - 1;
-      for (int which = tid == 0 && ragged_first ? 0 : 1; which < (tid == last % THREADS && ragged_last ? 2 : 1); ++which)
-        for (int i = 0; i < W; ++i) {
-          const int q = (which ? last * W : 0) + i;
-          const T v = q < s || q >= end ? from_f<T>(-INFINITY) : left ? z[q] : zs[q];
-          zs[q] = v;
-          sh_edge[par][which][i] = v;
+    __syncthreads();
+    if (tid == ISSUER)
+      for (int b = 0; b < nbuf && b < count; ++b) issue(sh_rows[b], (used + b) % nbuf);
+    if (warp == 1 && count > 0) {
+      fetch_teacher(sh_rows[0], 0);
+      teacher(0);
+      if (count > 1) fetch_teacher(sh_rows[1], 1);
+    }
+    for (int at = 0; at < count; ++at, ++used) {
+      const int row = sh_rows[at], y = sh_ys[at], slot = at % SLOTS, par = at & 1, b = used % nbuf, s = shift_of(row);
+      T* out = grad + row * p.ldo - s;     // position q = s + column
+      const int end = s + V, nvec = (end + W - 1) / W, last = nvec - 1;
+      tc::mbar_wait(tc::smem_u32(&bars[b]), (uint32_t)(used / nbuf) & 1u, &sh_abort, status, 81);
+      T* zs = reinterpret_cast<T*>(smem + (size_t)b * buf_bytes);
+      // A ragged first or last vector (in the first and last row of all the copies left it out): the thread that owns it keeps its
+      // logits for the gradient and puts -inf around them.
+      const bool ragged_first = s > 0 || (last == 0 && end % W != 0), ragged_last = end % W != 0;
+      if ((tid == 0 && ragged_first) || (tid == last % THREADS && ragged_last)) {
+        const T* z = logits + row * p.ld - s;
+        const bool left = row == 0 || row == M - 1;
+        for (int which = tid == 0 && ragged_first ? 0 : 1; which < (tid == last % THREADS && ragged_last ? 2 : 1); ++which)
+          for (int i = 0; i < W; ++i) {
+            const int q = (which ? last * W : 0) + i;
+            const T v = q < s || q >= end ? from_f<T>(-INFINITY) : left ? z[q] : zs[q];
+            zs[q] = v;
+            sh_edge[par][which][i] = v;
+          }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");   // before a copy takes the buffer again
+      }
+      // ---- this thread's maximum, then its exponentials relative to it
+      float m = -INFINITY;
+      if constexpr (W == 8) {
+        __nv_bfloat162 m2 = __floats2bfloat162_rn(-INFINITY, -INFINITY);
+#pragma unroll 4
+        for (int v = tid; v < nvec; v += THREADS) {
+          Vec16<T> r; r.load(zs + (size_t)v * W);
+          const __nv_bfloat162* h2 = reinterpret_cast<const __nv_bfloat162*>(&r.raw);
+          m2 = __hmax2(m2, __hmax2(__hmax2(h2[0], h2[1]), __hmax2(h2[2], h2[3])));
         }
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // before a copy takes the buffer again
-    }
-    // ---- this thread's maximum, then its exponentials relative to it
-    float m = -INFINITY;
-    if constexpr (W == 8) {
-      __nv_bfloat162 m2 = __floats2bfloat162_rn(-INFINITY, -INFINITY);
+        m = fmaxf(__low2float(m2), __high2float(m2));
+      } else {
 #pragma unroll 4
-      for (int v = tid; v < nvec; v += THREADS) {
-        Vec16<T> r; r.load(zs + (size_t)v * W);
-        const __nv_bfloat162* h2 = reinterpret_cast<const __nv_bfloat162*>(&r.raw);
-        m2 = __hmax2(m2, __hmax2(__hmax2(h2[0], h2[1]), __hmax2(h2[2], h2[3])));
-      }
-      m = fmaxf(__low2float(m2), __high2float(m2));
-    } else {
-#pragma unroll 4
-      for (int v = tid; v < nvec; v += THREADS) {
-        Vec16<T> r; r.load(zs + (size_t)v * W);
+        for (int v = tid; v < nvec; v += THREADS) {
+          Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
-        for (int i = 0; i < W; ++i) m = fmaxf(m, r.get(i));
+          for (int i = 0; i < W; ++i) m = fmaxf(m, r.get(i));
+        }
       }
-    }
-    const float mine = m == -INFINITY ? 0.f : m;
-    uint64_t sT2 = 0ull, s12 = 0ull;
-    const uint64_t cT2 = tc::pack2(p.cT, p.cT), c12 = tc::pack2(p.c1, p.c1);
-    {
-      const uint64_t neg2 = tc::pack2(-mine, -mine);
-#pragma unroll 2
-      for (int v = tid; v < nvec; v += THREADS) {
-        Vec16<T> r; r.load(zs + (size_t)v * W);
+      const float mine = m == -INFINITY ? 0.f : m;
+      uint64_t sT2 = 0ull, s12 = 0ull;
+      {
+        const uint64_t neg2 = tc::pack2(-mine, -mine);
+#pragma unroll 4
+        for (int v = tid; v < nvec; v += THREADS) {
+          Vec16<T> r; r.load(zs + (size_t)v * W);
+#pragma unroll
+          for (int i = 0; i < W / 2; ++i) {
+            const uint64_t dd = add2(pair_of(r, i), neg2);       // z - maximum
+            const uint64_t e = exp_pair(tc::mul2(dd, cT2));
+            sT2 = add2(sT2, e);
+            if constexpr (MODE == EXP_HALF) s12 = tc::fma2(e, e, s12);
+            if constexpr (MODE == EXP_TWO) s12 = add2(s12, exp_pair(tc::mul2(dd, c12)));
+          }
+        }
+      }
+      float sT, s1;
+      {
+        float a, c;
+        tc::unpack2(sT2, a, c); sT = a + c;
+        tc::unpack2(s12, a, c); s1 = a + c;
+      }
+      // ---- the row's maximum and sums.  Without a maximum the sums are 0 or, from NaN, NaN: no factor
+      auto factor = [&](float from, float to, float c) { return from == -INFINITY ? 1.f : ex2((from - to) * c); };
+      const float wm = warp_max_redux(m), wbase = wm == -INFINITY ? 0.f : wm;
+      {
+        const float f = factor(m, wbase, p.cT);
+        sT = warp_sum(sT * f);
+        if constexpr (MODE == EXP_HALF) s1 = warp_sum(s1 * (f * f));
+        if constexpr (MODE == EXP_TWO) s1 = warp_sum(s1 * factor(m, wbase, p.c1));
+      }
+      if (lane == 0) {
+        sh_m[par][warp] = wm; sh_sT[par][warp] = sT;
+        if constexpr (MODE != EXP_ONE) sh_s1[par][warp] = s1;
+      }
+      __syncthreads();
+      if (tid == ISSUER && nbuf > 1 && at > 0 && at + 1 < count) issue(sh_rows[at + 1], (used + 1) % nbuf);    // nobody reads the previous row's logits any more
+      float base;
+      {
+        float rm = sh_m[par][lane % NW];
+        sT = sh_sT[par][lane % NW];
+        s1 = MODE == EXP_ONE ? 0.f : sh_s1[par][lane % NW];
+        m = warp_max_redux(rm);
+        base = m == -INFINITY ? 0.f : m;
+        const float f = factor(rm, base, p.cT);
+        sT *= f;
+        if constexpr (MODE == EXP_HALF) s1 *= f * f;
+        if constexpr (MODE == EXP_TWO) s1 *= factor(rm, base, p.c1);
+#pragma unroll
+        for (int o = NW / 2; o > 0; o >>= 1) {
+          sT += __shfl_xor_sync(0xffffffffu, sT, o);
+          if constexpr (MODE != EXP_ONE) s1 += __shfl_xor_sync(0xffffffffu, s1, o);
+        }
+        if constexpr (MODE == EXP_ONE) s1 = sT;
+      }
+      const float wkT = sh_teach[slot] ? p.wk * p.temp : 0.f;
+      const float f1 = MODE == EXP_ONE ? (p.wc + wkT) / s1 * inv_n : p.wc / s1 * inv_n, fT = MODE == EXP_ONE ? 0.f : wkT / sT * inv_n;
+      if (warp == 0) {                     // the divergence, the row's loss, and what its targets need
+        const float log_sT = logf(sT), tmax = sh_tmax[slot], lts = sh_lts[slot], *t = p.t + (int64_t)row * k;
+        float kl = 0.f;
+        for (int j = lane; j < k; j += 32) {
+          const int v = sh_idx[slot][j];
+          const float q = sh_q[slot][j], z = v >= 0 ? to_f<T>(zs[s + v]) : 0.f;
+          sh_z[par][j] = z;
+          // T times the divergence: (z - base) / T could overflow
+          if (q != 0.f) kl += q * fmaf(p.temp, ((t[j] - tmax) * p.inv_t - lts) + log_sT, base - z);
+        }
+        kl = warp_sum(kl);
+        if (lane == 0) {
+          const float zy = p.labels ? to_f<T>(zs[s + y]) : 0.f;
+          float r = wkT != 0.f ? p.wk * p.temp * kl : 0.f;
+          if (p.wc != 0.f) r += p.wc * (logf(s1) - (zy - base));
+          p.rows[row] = r;
+          sh_zy[par] = zy; sh_f1[par] = f1; sh_fT[par] = fT; sh_base[par] = base; sh_fq[par] = wkT * inv_n;
+        }
+      } else if (warp == 1) {
+        if (lane < 2 * W) {                // the ragged ends, one logit per lane
+          const int which = lane / W, i = lane % W, q = (which ? last * W : 0) + i;
+          if ((which ? ragged_last : ragged_first && !(last == 0 && ragged_last)) && q >= s && q < end) {
+            const float z = to_f<T>(sh_edge[par][which][i]) - base, x = ex2(z * p.cT);
+            out[q] = from_f<T>(MODE == EXP_ONE ? f1 * x : MODE == EXP_HALF ? x * fmaf(x, f1, fT) : fmaf(f1, ex2(z * p.c1), fT * x));
+          }
+        }
+        __syncwarp();
+        if (at + 1 < count) teacher((at + 1) % SLOTS);
+        if (at + 2 < count) fetch_teacher(sh_rows[at + 2], (at + 2) % SLOTS);
+      } else if (at > 0) {
+        write_targets(sh_rows[at - 1], sh_ys[at - 1], (at - 1) % SLOTS, par ^ 1);
+      }
+      // ---- gradient
+      const uint64_t f12 = tc::pack2(f1, f1), fT2 = tc::pack2(fT, fT), neg2 = tc::pack2(-base, -base);
+      const int v_to = ragged_last ? last : nvec;
+#pragma unroll 4
+      for (int v = tid == 0 && ragged_first ? THREADS : tid; v < v_to; v += THREADS) {
+        Vec16<T> r, o;
+        r.load(zs + (size_t)v * W);
 #pragma unroll
         for (int i = 0; i < W / 2; ++i) {
-          const uint64_t dd = add2(pair_of(r, i), neg2);         // z - maximum
+          const uint64_t dd = add2(pair_of(r, i), neg2);
           const uint64_t e = exp_pair(tc::mul2(dd, cT2));
-          sT2 = add2(sT2, e);
-          if constexpr (MODE == EXP_HALF) s12 = tc::fma2(e, e, s12);
-          if constexpr (MODE == EXP_TWO) s12 = add2(s12, exp_pair(tc::mul2(dd, c12)));
+          uint64_t w;
+          if constexpr (MODE == EXP_ONE) w = tc::mul2(e, f12);
+          if constexpr (MODE == EXP_HALF) w = tc::mul2(e, tc::fma2(e, f12, fT2));
+          if constexpr (MODE == EXP_TWO) w = tc::fma2(e, fT2, tc::mul2(f12, exp_pair(tc::mul2(dd, c12))));
+          float a, c;
+          tc::unpack2(w, a, c);
+          if constexpr (W == 8) reinterpret_cast<__nv_bfloat162*>(&o.raw)[i] = __floats2bfloat162_rn(a, c);
+          else { o.set(2 * i, a); o.set(2 * i + 1, c); }
         }
-      }
-    }
-    float sT, s1;
-    {
-      float a, c;
-      tc::unpack2(sT2, a, c); sT = a + c;
-      tc::unpack2(s12, a, c); s1 = a + c;
-    }
-    // ---- warp 0: the teacher's distribution
-    float tsum = 0.f, tmax = -INFINITY;
-    if (warp == 0) {
-      const bool left = row == 0 || row == M - 1;        // another thread's patch may not be visible yet: the logits themselves
-      for (int j = lane; j < k; j += 32) {
-        const int v = sh_idx[slot][j];
-        const bool ok = v >= 0 && v < V;
-        const float t = ok ? sh_q[slot][j] : -INFINITY;
-        if (!ok) sh_idx[slot][j] = -1;
-        sh_q[slot][j] = t;
-        sh_z[slot][j] = !ok ? 0.f : to_f<T>(left ? logits[row * p.ld + v] : zs[s + v]);
-        tmax = t != t || tmax != tmax ? __uint_as_float(0x7fffffffu) : fmaxf(tmax, t);
-      }
-      for (int j = k + lane; j < (k + 3) / 4 * 4; j += 32) sh_idx[slot][j] = -1;
-      const bool nan = __any_sync(0xffffffffu, tmax != tmax);
-      tmax = nan ? __uint_as_float(0x7fffffffu) : warp_max(tmax);
-      for (int j = lane; j < k; j += 32) tsum += expf((sh_q[slot][j] - tmax) * p.inv_t);       // not used where tmax is -inf
-      tsum = warp_sum(tsum);
-      if (lane == 0) {
-        sh_zy[slot] = p.labels ? to_f<T>(left ? logits[row * p.ld + y] : zs[s + y]) : 0.f;
-        sh_teach[slot] = tmax != -INFINITY && p.wk != 0.f;     // else the teacher says nothing about this row
-      }
-    }
-    // ---- the row's maximum and sums.  Without a maximum the sums are 0 or, from NaN, NaN: no factor
-    auto factor = [&](float from, float to, float c) { return from == -INFINITY ? 1.f : ex2((from - to) * c); };
-    const float wm = warp_max(m), wbase = wm == -INFINITY ? 0.f : wm;
-    {
-      const float f = factor(m, wbase, p.cT);
-      sT = warp_sum(sT * f);
-      if constexpr (MODE == EXP_HALF) s1 = warp_sum(s1 * (f * f));
-      if constexpr (MODE == EXP_TWO) s1 = warp_sum(s1 * factor(m, wbase, p.c1));
-    }
-    if (lane == 0) {
-      sh_m[par][warp] = wm; sh_sT[par][warp] = sT;
-      if constexpr (MODE != EXP_ONE) sh_s1[par][warp] = s1;
-    }
-    __syncthreads();
-    if (tid == ISSUER && nbuf > 1 && done > 0) issue_next();           // nobody reads the previous row's logits any more
-    if (done > 0 && warp >= 2) write_targets(slot == 0 ? SLOTS - 1 : slot - 1);
-    ++done;
-    {
-      const float rm = lane < NW ? sh_m[par][lane] : -INFINITY;
-      m = warp_max(rm);
-      const float base = m == -INFINITY ? 0.f : m, f = factor(rm, base, p.cT);
-      sT = warp_sum(lane < NW ? sh_sT[par][lane] * f : 0.f);
-      if constexpr (MODE == EXP_HALF) s1 = warp_sum(lane < NW ? sh_s1[par][lane] * (f * f) : 0.f);
-      else if constexpr (MODE == EXP_TWO) s1 = warp_sum(lane < NW ? sh_s1[par][lane] * factor(rm, base, p.c1) : 0.f);
-      else s1 = sT;
-    }
-    const float base = m == -INFINITY ? 0.f : m;
-    const bool teach = sh_teach[slot] != 0;
-    const float wkT = teach ? p.wk * p.temp : 0.f;
-    const float f1 = MODE == EXP_ONE ? (p.wc + wkT) / s1 * p.inv_n : p.wc / s1 * p.inv_n, fT = MODE == EXP_ONE ? 0.f : wkT / sT * p.inv_n;
-    // ---- warp 0: the divergence, the row's loss, and what its targets need
-    if (warp == 0) {
-      const float log_s1 = logf(s1), log_sT = logf(sT), log_ts = logf(tsum);
-      float kl = 0.f;
-      for (int j = lane; j < k; j += 32) {
-        const float lq = (sh_q[slot][j] - tmax) * p.inv_t - log_ts;
-        const float q = teach ? expf(lq) : 0.f;
-        if (q != 0.f) kl += q * fmaf(p.temp, lq + log_sT, base - sh_z[slot][j]);      // T times the divergence: (z - base) / T could overflow
-        sh_q[slot][j] = q;
-      }
-      kl = warp_sum(kl);
-      if (lane == 0) {
-        float r = teach ? p.wk * p.temp * kl : 0.f;
-        if (p.wc != 0.f) r += p.wc * (log_s1 - (sh_zy[slot] - base));
-        p.rows[row] = r;
-        sh_f1[slot] = f1; sh_fT[slot] = fT; sh_base[slot] = base; sh_fq[slot] = wkT * p.inv_n;
-        sh_row[slot] = row; sh_y[slot] = p.labels ? y : -1;
-      }
-      fetch_teacher(row + gridDim.x, slot == SLOTS - 1 ? 0 : slot + 1);
-    }
-    // ---- gradient
-    const uint64_t f12 = tc::pack2(f1, f1), fT2 = tc::pack2(fT, fT), neg2 = tc::pack2(-base, -base);
-    if (warp == 1 && lane < 2 * W) {       // the ragged ends, one logit per lane
-      const int which = lane / W, i = lane % W, q = (which ? last * W : 0) + i;
-      if ((which ? ragged_last : ragged_first && !(last == 0 && ragged_last)) && q >= s && q < end) {
-        const float z = to_f<T>(sh_edge[par][which][i]) - base, x = ex2(z * p.cT);
-        out[q] = from_f<T>(MODE == EXP_ONE ? f1 * x : MODE == EXP_HALF ? x * fmaf(x, f1, fT) : fmaf(f1, ex2(z * p.c1), fT * x));
-      }
-    }
-    const int v_to = ragged_last ? last : nvec;
-#pragma unroll 2
-    for (int v = tid == 0 && ragged_first ? THREADS : tid; v < v_to; v += THREADS) {
-      Vec16<T> r, o;
-      r.load(zs + (size_t)v * W);
+        if (p.same) o.store(out + (int64_t)v * W);
+        else
 #pragma unroll
-      for (int i = 0; i < W / 2; ++i) {
-        const uint64_t dd = add2(pair_of(r, i), neg2);
-        const uint64_t e = exp_pair(tc::mul2(dd, cT2));
-        uint64_t w;
-        if constexpr (MODE == EXP_ONE) w = tc::mul2(e, f12);
-        if constexpr (MODE == EXP_HALF) w = tc::mul2(e, tc::fma2(e, f12, fT2));
-        if constexpr (MODE == EXP_TWO) w = tc::fma2(e, fT2, tc::mul2(f12, exp_pair(tc::mul2(dd, c12))));
-        float a, c;
-        tc::unpack2(w, a, c);
-        if constexpr (W == 8) reinterpret_cast<__nv_bfloat162*>(&o.raw)[i] = __floats2bfloat162_rn(a, c);
-        else { o.set(2 * i, a); o.set(2 * i + 1, c); }
+          for (int i = 0; i < W; ++i) out[v * W + i] = reinterpret_cast<const T*>(&o.raw)[i];
       }
-      if (p.same) o.store(out + (int64_t)v * W);
-      else
-#pragma unroll
-        for (int i = 0; i < W; ++i) out[v * W + i] = reinterpret_cast<const T*>(&o.raw)[i];
+      if (p.ldo > V) zeros(out, end, s + (int)p.ldo);
+      if (nbuf == 1) {
+        __syncthreads();
+        if (tid == ISSUER && at + 1 < count) issue(sh_rows[at + 1], 0);
+      }
     }
-    if (out_end > end) zeros(end, out_end);
-    if (nbuf == 1) {
+    if (count > 0) {
       __syncthreads();
-      if (tid == ISSUER) issue_next();
+      if (warp >= 2) write_targets(sh_rows[count - 1], sh_ys[count - 1], (count - 1) % SLOTS, (count - 1) & 1);
     }
-    slot = slot == SLOTS - 1 ? 0 : slot + 1;
-  }
-  if (done > 0) {
-    __syncthreads();
-    if (warp >= 2) write_targets(slot == 0 ? SLOTS - 1 : slot - 1);
   }
 }
 
@@ -599,11 +625,10 @@ namespace {
 
 // Rows up to this many labels are counted by every block of the ring kernel instead of a launch in front of it.
 constexpr int COUNT_HERE = 4096;
-constexpr int RING_TABLES = 11264, RING_BYTES = 232448 - 1024 - RING_TABLES;     // static tables; dynamic shared memory of all blocks of an SM
+constexpr int RING_TABLES = 12800, RING_BYTES = 232448 - 1024 - RING_TABLES;     // static tables; dynamic shared memory of all blocks of an SM
 
-template <typename T, int THREADS, int MODE>
+template <typename T, int THREADS, int MINB, int MODE>
 cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, int buf, int nbuf, int fit, int* status, cudaStream_t st) {
-  constexpr int MINB = 1024 / THREADS;
   const auto kernel = distill_ring_kernel<T, THREADS, MINB, MODE>;
   static PerDeviceOnce once;
   const int dev = current_device();
@@ -616,17 +641,17 @@ cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, i
   return launch_overlapped(kernel, dim3((unsigned)(M < most ? M : most)), dim3(THREADS), (size_t)nbuf * buf, st, logits, grad, p, M, nbuf, buf, status);
 }
 
-// As many rows per SM as shared memory holds, up to eight, and 1024 threads for all of them; two buffers per row where eight
-// rows have room for them.
+// As many rows per SM as shared memory holds, up to eight; two buffers per row where eight rows have room for them.
 template <typename T, int MODE>
 cudaError_t ring(const T* logits, T* grad, const DistillArgs& p, int M, int* status, cudaStream_t st) {
   const int buf = (int)(((size_t)p.V * sizeof(T) + 15) / 16 * 16 + 16);
   const int one = (RING_BYTES + RING_TABLES) / (buf + RING_TABLES), two = (RING_BYTES + RING_TABLES) / (2 * buf + RING_TABLES);
-  if (two >= 8) return launch_ring<T, 128, MODE>(logits, grad, p, M, buf, 2, two, status, st);
-  if (one >= 6) return launch_ring<T, 128, MODE>(logits, grad, p, M, buf, 1, one, status, st);
-  if (one >= 3) return launch_ring<T, 256, MODE>(logits, grad, p, M, buf, 1, one, status, st);
-  if (one == 2) return launch_ring<T, 512, MODE>(logits, grad, p, M, buf, 1, one, status, st);
-  return launch_ring<T, 1024, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  if (two >= 8) return launch_ring<T, 128, 8, MODE>(logits, grad, p, M, buf, 2, two, status, st);
+  if (one >= 6) return launch_ring<T, 128, 8, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  if (one >= 4) return launch_ring<T, 128, 5, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  if (one == 3) return launch_ring<T, 256, 3, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  if (one == 2) return launch_ring<T, 256, 2, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  return launch_ring<T, 512, 1, MODE>(logits, grad, p, M, buf, 1, one, status, st);
 }
 
 }  // namespace
@@ -635,7 +660,7 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
                     float temperature, float wc, float wk, int normalizer, void* grad, int64_t ldo, float* rows, int* n_valid, float* loss,
                     int* status, cudaStream_t st) {
   DistillArgs p;
-  p.labels = labels; p.idx = idx; p.t = t; p.ld = ld; p.ldo = ldo; p.V = V; p.k = k; p.temp = temperature; p.inv_t = 1.0f / temperature; p.inv_n = 0.f; p.wc = wc; p.wk = wk; p.rows = rows;
+  p.labels = labels; p.idx = idx; p.t = t; p.ld = ld; p.ldo = ldo; p.V = V; p.k = k; p.temp = temperature; p.inv_t = 1.0f / temperature; p.wc = wc; p.wk = wk; p.rows = rows;
   const bool count = labels != nullptr && normalizer <= 0;
   p.n_valid = count ? n_valid : nullptr;
   p.n_fixed = normalizer > 0 ? normalizer : M;
