@@ -35,11 +35,6 @@ constexpr uint32_t IDESC_64KK = make_idesc(BT, DH);                   // [128 x 
 constexpr uint32_t IDESC_64MN = make_idesc(BT, DH) | (1u << 16);      // [128 x 64] products, right operand MN-major
 constexpr float LOG2E = 1.4426950408889634f;
 
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 // 16 consecutive tensor-memory columns of this thread's lane
 __device__ __forceinline__ void tc_ld16(uint32_t taddr, float* v) {
   uint32_t* r = reinterpret_cast<uint32_t*>(v);

@@ -247,11 +247,6 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b) {
-  uint64_t d;
-  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-  return d;
-}
 // the W values of a 16-byte vector as W / 2 packed pairs
 __device__ __forceinline__ uint64_t pair_of(const Vec16<bf16>& r, int i) { return tc::bf16x2_to_f32x2(reinterpret_cast<const uint32_t*>(&r.raw)[i]); }
 __device__ __forceinline__ uint64_t pair_of(const Vec16<float>& r, int i) { return tc::pack2(r.get(2 * i), r.get(2 * i + 1)); }
@@ -471,11 +466,11 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
           Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
           for (int i = 0; i < W / 2; ++i) {
-            const uint64_t dd = add2(pair_of(r, i), neg2);       // z - maximum
+            const uint64_t dd = tc::add2(pair_of(r, i), neg2);       // z - maximum
             const uint64_t e = exp_pair(tc::mul2(dd, cT2));
-            sT2 = add2(sT2, e);
+            sT2 = tc::add2(sT2, e);
             if constexpr (MODE == EXP_HALF) s12 = tc::fma2(e, e, s12);
-            if constexpr (MODE == EXP_TWO) s12 = add2(s12, exp_pair(tc::mul2(dd, c12)));
+            if constexpr (MODE == EXP_TWO) s12 = tc::add2(s12, exp_pair(tc::mul2(dd, c12)));
           }
         }
       }
@@ -561,7 +556,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
         r.load(zs + (size_t)v * W);
 #pragma unroll
         for (int i = 0; i < W / 2; ++i) {
-          const uint64_t dd = add2(pair_of(r, i), neg2);
+          const uint64_t dd = tc::add2(pair_of(r, i), neg2);
           const uint64_t e = exp_pair(tc::mul2(dd, cT2));
           uint64_t w;
           if constexpr (MODE == EXP_ONE) w = tc::mul2(e, f12);

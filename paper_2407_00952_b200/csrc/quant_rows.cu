@@ -7,50 +7,107 @@
 // collects sum s^2 and max |s g| together and every rounding decision is one of fp32 products and one fp32 division, whatever
 // the order of the sum.  All arithmetic is fp32; h and y are rounded once to the buffers' type, the norm sees s before that.
 // Bounded by HBM: a row lives in registers between its reduction and its output (4 accesses of 16 bytes per thread; 1 to 32 lanes
-// per row up to 128 accesses, else whole warps, up to 1024 threads), so it is read once.  Maxima are taken on the bits of |v| as
-// unsigned integers: a NaN or infinity is larger than every finite value.
+// per row up to 128 accesses, else whole warps, up to 1024 threads), so it is read once.  Rows are many and short-lived: a block
+// each (walking the rows with copies one row ahead was 10-20 % slower where no sums are carried from row to row). 
 // FRAME: rows that do not start on 16-byte boundaries (odd widths in contiguous rows).  A row is then the whole 16-byte vectors in
 // it, position q = column + shift, and the elements around them, which are taken one by one; the gain and the factors, which start
 // at column 0, are read as words and shifted, and the codes turn back to column 0 through shared memory.
-#include <algorithm>
-
 #include "common.cuh"
 #include "host_common.h"
 #include "kernels.h"
 #include "launch.cuh"
+#include "tc_common.cuh"
 
 namespace sl {
 namespace {
 
 constexpr float TINY_ROW = 1e-36f;       // below this 127 / max overflows: the row is held as zero
 constexpr int NV = 4;                    // accesses of 16 bytes per thread
+// Rows on 16-byte boundaries; at any place, but all arrays of activations at the same place of a 16-byte vector; at any place.
+enum { FRAME_NONE = 0, FRAME_SAME = 1, FRAME_ANY = 2 };
 
-__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+using tc::add2; using tc::fma2; using tc::mul2; using tc::pack2; using tc::unpack2;
+
+// The values of a 16-byte vector as pairs of floats: the arithmetic runs on the packed fp32 instructions, which halve its
+// instructions (a norm is bound by instruction issue as much as by HBM: 35 instructions per element of one value at a time, 57 us for
+// 8192 x 4096 bf16 with residual and both outputs).
+template <typename T> struct Pairs { uint64_t v[Vec16<T>::N / 2]; };
+__device__ __forceinline__ Pairs<bf16> pairs_of(const Vec16<bf16>& r) {
+  const uint32_t w[4] = {r.raw.x, r.raw.y, r.raw.z, r.raw.w};
+  Pairs<bf16> p;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) p.v[i] = tc::bf16x2_to_f32x2(w[i]);
+  return p;
+}
+__device__ __forceinline__ Pairs<float> pairs_of(const Vec16<float>& r) {
+  Pairs<float> p;
+  p.v[0] = pack2(r.raw.x, r.raw.y);
+  p.v[1] = pack2(r.raw.z, r.raw.w);
+  return p;
+}
+__device__ __forceinline__ Vec16<bf16> vector_of(const Pairs<bf16>& p) {
+  uint32_t w[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a, b;
+    unpack2(p.v[i], a, b);
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    w[i] = *reinterpret_cast<const uint32_t*>(&h);
+  }
+  Vec16<bf16> r;
+  r.raw = make_uint4(w[0], w[1], w[2], w[3]);
+  return r;
+}
+__device__ __forceinline__ Vec16<float> vector_of(const Pairs<float>& p) {
+  Vec16<float> r;
+  unpack2(p.v[0], r.raw.x, r.raw.y);
+  unpack2(p.v[1], r.raw.z, r.raw.w);
+  return r;
+}
+
+// The larger of `top` and both magnitudes of a pair; a NaN stays.
+__device__ __forceinline__ float max_abs(float top, uint64_t pair) {
+  float a, b, r;
+  unpack2(pair, a, b);
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(top), "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float max_abs(float top, float v) {
+  float r;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(top), "f"(fabsf(v)));
+  return r;
+}
 
 // rint(v * inv) for |v * inv| < 128 in the low byte of the result: the product is rounded to fp32 first, then adding 1.5 * 2^23
 // leaves the nearest integer (ties to even) in the low bits of the sum.
-__device__ __forceinline__ uint32_t code_bits(float v, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(v, inv), 12582912.0f)); }
-// W codes as W / 4 words
-template <int W> __device__ __forceinline__ void code_words(uint32_t* w, const float* v, float inv, bool live) {
+constexpr float ROUNDER = 12582912.0f;
+__device__ __forceinline__ uint32_t code_bits(float v, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(v, inv), ROUNDER)); }
+// Four of them.  The sums are scalar: a packed product and a packed sum are contracted into one rounding, .rn or not.
+__device__ __forceinline__ uint32_t code_word(uint64_t v01, uint64_t v23, uint64_t inv2, bool live) {
+  float a, b, c, d;
+  unpack2(mul2(v01, inv2), a, b);
+  unpack2(mul2(v23, inv2), c, d);
+  const uint32_t lo = __byte_perm(__float_as_uint(__fadd_rn(a, ROUNDER)), __float_as_uint(__fadd_rn(b, ROUNDER)), 0x0040);
+  const uint32_t hi = __byte_perm(__float_as_uint(__fadd_rn(c, ROUNDER)), __float_as_uint(__fadd_rn(d, ROUNDER)), 0x0040);
+  return live ? __byte_perm(lo, hi, 0x5410) : 0u;
+}
+// the W codes of a vector as W / 4 words
+template <typename T> __device__ __forceinline__ void code_words(uint32_t* w, const Pairs<T>& v, float inv, bool live) {
+  const uint64_t inv2 = pack2(inv, inv);
 #pragma unroll
-  for (int i = 0; i < W / 4; ++i) {
-    const uint32_t lo = __byte_perm(code_bits(v[4 * i], inv), code_bits(v[4 * i + 1], inv), 0x0040);
-    const uint32_t hi = __byte_perm(code_bits(v[4 * i + 2], inv), code_bits(v[4 * i + 3], inv), 0x0040);
-    w[i] = live ? __byte_perm(lo, hi, 0x5410) : 0u;
-  }
+  for (int i = 0; i < Vec16<T>::N / 4; ++i) w[i] = code_word(v.v[2 * i], v.v[2 * i + 1], inv2, live);
 }
 template <int W> __device__ __forceinline__ void store_words(void* p, const uint32_t* w) {
   if constexpr (W == 8) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
   else *reinterpret_cast<uint32_t*>(p) = w[0];
 }
 
-// The largest magnitude's bits -> what a row's codes and scale need.  `unit` is what one unit of the maximum stands for
-// (rstd for a norm, 1 for plain rows).
+// The largest magnitude -> what a row's codes and scale need.  `unit` is what one unit of the maximum stands for (rstd for a norm,
+// 1 for plain rows).
 struct RowScale { float inv, scale; bool live; };
-__device__ __forceinline__ RowScale row_scale(uint32_t top_bits, float unit) {
+__device__ __forceinline__ RowScale row_scale(float a, float unit) {
   RowScale r;
-  const float a = __uint_as_float(top_bits);
-  const bool finite = top_bits < 0x7f800000u;
+  const bool finite = a < INFINITY;        // neither infinity nor NaN
   r.live = finite && a >= TINY_ROW;
   r.inv = r.live ? __fdiv_rn(127.0f, a) : 0.f;
   r.scale = r.live ? __fdiv_rn(__fmul_rn(a, unit), 127.0f) : finite ? 0.f : __uint_as_float(0x7fffffffu);
@@ -71,7 +128,8 @@ struct Place {
 // Sums and maximum over the threads of a row.  With whole warps per row every thread of the block takes part, in step; two sets of
 // shared memory in turn make one barrier per call enough.
 struct RowShared { float sum[2][32]; uint32_t top[32]; };
-template <int NS, bool MAX> __device__ __forceinline__ void reduce_row(float* s, uint32_t& top, const Place& at, RowShared* sh) {
+template <int NS, bool MAX> __device__ __forceinline__ void reduce_row(float* s, float& largest, const Place& at, RowShared* sh) {
+  uint32_t top = MAX ? __float_as_uint(largest) : 0u;    // no negative values: the order of the bits, NaN above all
   const int lanes = at.n < 32 ? at.n : 32;
   for (int o = lanes >> 1; o > 0; o >>= 1) {
 #pragma unroll
@@ -90,11 +148,12 @@ template <int NS, bool MAX> __device__ __forceinline__ void reduce_row(float* s,
     for (int k = 0; k < NS; ++k) s[k] = warp_sum(lane < nw ? sh->sum[k][first + lane] : 0.f);
     if constexpr (MAX) top = __reduce_max_sync(0xffffffffu, lane < nw ? sh->top[first + lane] : 0u);
   }
+  if constexpr (MAX) largest = __uint_as_float(top);
 }
 
 // A row of d elements at positions s .. s + d: whole vectors [v0, v1), and `edges` elements around them.  (The last vector before the
 // row's end counts as edges: reading the gain of a whole vector may take in the element behind it.)
-template <typename T, bool FRAME> struct Span {
+template <typename T, int FRAME> struct Span {
   static constexpr int W = Vec16<T>::N;
   int s, d, v0, v1, head, edges;
   __device__ __forceinline__ Span(const T* row, int width) : s(0), d(width), v0(0), v1(width / W), head(0), edges(0) {
@@ -109,32 +168,97 @@ template <typename T, bool FRAME> struct Span {
   }
   __device__ __forceinline__ int edge(int e) const { return e < head ? e : v1 * W + (e - head) - s; }     // column of the e-th
   __device__ __forceinline__ int column(int v) const { return v * W - s; }
-  __device__ __forceinline__ bool fits(const T* row) const { return !FRAME || ((reinterpret_cast<uintptr_t>(row - s) & 15u) == 0); }
 };
 
-// Vector v of a row that has whole vectors there; fits: its vectors are 16-byte aligned as those of the span's row are.
-template <typename T, bool FRAME> __device__ __forceinline__ void load_row(Vec16<T>& r, const T* row, const Span<T, FRAME>& f, int v, bool fits) {
-  const T* p = row + f.column(v);
-  if (!FRAME || fits) r.load(p);
-  else {
-#pragma unroll
-    for (int i = 0; i < Vec16<T>::N; ++i) reinterpret_cast<T*>(&r.raw)[i] = p[i];
+// What a thread reads of a row: its vectors, and its edge (FRAME: one at most).  AHEAD: one row ahead, the vectors through shared memory
+// (slots of its own, so nothing but its own copies is waited for; stages: two rows, or one where there is no more room), the edge
+// through a register.  Else straight from memory.  FRAME_ANY: arrays whose rows are not 16-byte aligned where the first array's
+// are, element by element.
+template <typename T, int FRAME, int ARRAYS, bool AHEAD, int EARLY = ARRAYS> struct Feed {
+  const T* p[ARRAYS];
+  bool fit[ARRAYS];
+  T edge[ARRAYS], edge_next[ARRAYS];
+  Vec16<T> raw[AHEAD ? 1 : EARLY][AHEAD ? 1 : NV];
+  int stages, stage;
+  uint8_t* slots;
+  __device__ __forceinline__ Feed(int st, uint8_t* smem) : stages(st), stage(0), slots(smem + threadIdx.x * 16) {}
+  __device__ __forceinline__ void array(int a, const T* q) {
+    p[a] = q;
+    fit[a] = FRAME != FRAME_ANY || ((reinterpret_cast<uintptr_t>(q) - reinterpret_cast<uintptr_t>(p[0])) & 15u) == 0;
   }
-}
-template <typename T, bool FRAME> __device__ __forceinline__ void store_row(T* row, const Span<T, FRAME>& f, int v, bool fits, const float* x) {
-  constexpr int W = Vec16<T>::N;
-  Vec16<T> r;
+  __device__ __forceinline__ uint8_t* slot(int st, int a, int k) const { return slots + (size_t)((st * ARRAYS + a) * NV + k) * blockDim.x * 16; }
+  __device__ __forceinline__ void fetch(int64_t row, int64_t M, int d, const Place& at, int st) {
+    if (row < M) {
+      const Span<T, FRAME> f(p[0] + row * d, d);
 #pragma unroll
-  for (int i = 0; i < W; ++i) r.set(i, x[i]);
+      for (int a = 0; a < ARRAYS; ++a) {
+        const T* q = p[a] + row * d;
+        if (!AHEAD && a < EARLY) {         // under way before the first use
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
+            const int v = f.v0 + k * at.n + at.t;
+            if (v < f.v1) read(raw[AHEAD || a >= EARLY ? 0 : a][AHEAD ? 0 : k], a, q + f.column(v));
+          }
+        }
+        if (FRAME && at.t < f.edges) edge_next[a] = q[f.edge(at.t)];
+        if constexpr (AHEAD) {
+          if (!fit[a]) continue;
+#pragma unroll
+          for (int k = 0; k < NV; ++k) {
+            const int v = f.v0 + k * at.n + at.t;
+            if (v < f.v1)
+              asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(slot(st, a, k))), "l"(q + f.column(v)) : "memory");
+          }
+        }
+      }
+    }
+    if (AHEAD) asm volatile("cp.async.commit_group;" ::: "memory");
+  }
+  __device__ __forceinline__ void read(Vec16<T>& r, int a, const T* q) const {
+    if (fit[a]) r.load(q);
+    else {
+#pragma unroll
+      for (int i = 0; i < Vec16<T>::N; ++i) reinterpret_cast<T*>(&r.raw)[i] = q[i];
+    }
+  }
+  // before the first row, at the begin of a row (whose successor is `next`), at its end
+  __device__ __forceinline__ void start(int64_t row, int64_t M, int d, const Place& at) { if (AHEAD) fetch(row, M, d, at, 0); }
+  __device__ __forceinline__ void begin(int64_t row, int64_t next, int64_t M, int d, const Place& at) {
+    if (!AHEAD) fetch(row, M, d, at, 0);
+#pragma unroll
+    for (int a = 0; a < ARRAYS; ++a) edge[a] = edge_next[a];
+    if (!AHEAD) return;
+    if (stages == 2) {
+      fetch(next, M, d, at, stage ^ 1);
+      asm volatile("cp.async.wait_group 1;" ::: "memory");
+    } else {
+      asm volatile("cp.async.wait_group 0;" ::: "memory");
+    }
+  }
+  __device__ __forceinline__ void end(int64_t next, int64_t M, int d, const Place& at) {
+    if (!AHEAD) return;
+    if (stages == 2) stage ^= 1;
+    else fetch(next, M, d, at, 0);
+  }
+  __device__ __forceinline__ void finish() const { if (AHEAD) asm volatile("cp.async.wait_group 0;" ::: "memory"); }
+  // vector v = k-th of this thread, of array a, in the row at q = p[a] + row * d
+  __device__ __forceinline__ void take(Vec16<T>& r, int a, int k, const T* q, int column) const {
+    if constexpr (!AHEAD) r = raw[a][k];
+    else if (fit[a]) r.raw = *reinterpret_cast<const decltype(r.raw)*>(slot(stage, a, k));
+    else read(r, a, q + column);
+  }
+};
+template <typename T, int FRAME> __device__ __forceinline__ void store_row(T* row, const Span<T, FRAME>& f, int v, bool fits, const Pairs<T>& x) {
+  const Vec16<T> r = vector_of(x);
   T* p = row + f.column(v);
-  if (!FRAME || fits) r.store(p);
+  if (FRAME != FRAME_ANY || fits) r.store(p);
   else {
 #pragma unroll
-    for (int i = 0; i < W; ++i) p[i] = reinterpret_cast<const T*>(&r.raw)[i];
+    for (int i = 0; i < Vec16<T>::N; ++i) p[i] = reinterpret_cast<const T*>(&r.raw)[i];
   }
 }
 // The gain at the columns of vector v.  Shifted bf16 pairs: words from the even element at or before the first, joined by twos.
-template <typename T, bool FRAME> __device__ __forceinline__ void load_gain(Vec16<T>& r, const T* g, const Span<T, FRAME>& f, int v) {
+template <typename T, int FRAME> __device__ __forceinline__ void load_gain(Vec16<T>& r, const T* g, const Span<T, FRAME>& f, int v) {
   constexpr int W = Vec16<T>::N;
   const int c = f.column(v);
   if constexpr (!FRAME) r.load(g + c);
@@ -154,24 +278,35 @@ template <typename T, bool FRAME> __device__ __forceinline__ void load_gain(Vec1
     for (int i = 0; i < W; ++i) r.set(i, __ldg(g + c + i));
   }
 }
-// x times the column factors of vector v (factor may be null)
-template <typename T, bool FRAME> __device__ __forceinline__ void scaled(float* o, const Vec16<T>& r, const float* factor, const Span<T, FRAME>& f, int v) {
+// x times the column factors of vector v (factor may be null).  Shifted factors: whole float4s around them, by the shift.
+template <typename T, int FRAME> __device__ __forceinline__ Pairs<T> scaled(const Vec16<T>& r, const float* factor, const Span<T, FRAME>& f, int v) {
   constexpr int W = Vec16<T>::N;
-#pragma unroll
-  for (int i = 0; i < W; ++i) o[i] = r.get(i);
+  Pairs<T> p = pairs_of(r);
   if (factor) {
-    const int c = f.column(v);
-    float w[W + 4];
-    if constexpr (!FRAME) {
+    const float* q = factor + f.column(v);
+    const int off = FRAME ? (int)((reinterpret_cast<uintptr_t>(q) >> 2) & 3u) : 0;
+    auto times = [&](const float* w) {
 #pragma unroll
-      for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(w + i) = __ldg(reinterpret_cast<const float4*>(factor + c + i));
+      for (int i = 0; i < W / 2; ++i) p.v[i] = mul2(p.v[i], pack2(w[2 * i], w[2 * i + 1]));
+    };
+    float w[W + 4];
+    if (off == 0) {
+#pragma unroll
+      for (int i = 0; i < W; i += 4) *reinterpret_cast<float4*>(w + i) = __ldg(reinterpret_cast<const float4*>(q + i));
+      times(w);
+    } else if (f.column(v) + W + 4 <= f.d && f.column(v) >= 4) {
+#pragma unroll
+      for (int i = 0; i <= W; i += 4) *reinterpret_cast<float4*>(w + i) = __ldg(reinterpret_cast<const float4*>(q - off + i));
+      if (off == 1) times(w + 1);
+      else if (off == 2) times(w + 2);
+      else times(w + 3);
     } else {
 #pragma unroll
-      for (int i = 0; i < W; ++i) w[i] = __ldg(factor + c + i);
+      for (int i = 0; i < W; ++i) w[i] = __ldg(q + i);
+      times(w);
     }
-#pragma unroll
-    for (int i = 0; i < W; ++i) o[i] = __fmul_rn(o[i], w[i]);
   }
+  return p;
 }
 
 // FRAME: the row's codes lie in shared memory at their positions (`mine`: 16-byte aligned, room for a word more); out with
@@ -187,69 +322,84 @@ __device__ __forceinline__ void codes_out(const uint8_t* mine, int8_t* cr, int s
   } else {
     for (int c = at.t; c < d; c += at.n) cr[c] = (int8_t)mine[s + c];
   }
+  if (at.n <= 32) __syncwarp();            // before the next row's codes (whole warps: its reduction's barrier)
 }
 // Shared memory of a row's codes, for `threads` threads.
 template <typename T> __host__ __device__ constexpr int code_bytes(int threads) { return (threads * NV * Vec16<T>::N + 4 * Vec16<T>::N + 31) / 16 * 16; }
 __device__ __forceinline__ uint8_t one_code(float v, const RowScale& rs) { return rs.live ? (uint8_t)code_bits(v, rs.inv) : (uint8_t)0; }
 
-template <typename T, bool FRAME>
+// The rows of a thread: its group's, every (groups of the grid)-th (most kernels are launched with a group for every row).  `lead`: the row of the block's first group, by which all its
+// threads go through the same number of rows.
+struct Walk {
+  int64_t row, lead, step;
+  __device__ __forceinline__ explicit Walk(const Place& at) {
+    const int per = blockDim.x / at.n;
+    lead = (int64_t)blockIdx.x * per;
+    row = lead + at.group;
+    step = (int64_t)gridDim.x * per;
+  }
+};
+
+template <typename T, int FRAME>
 __global__ void __launch_bounds__(1024)
 quantize_kernel(const T* __restrict__ x, const float* __restrict__ factor, int64_t M, int d, int threads, int8_t* __restrict__ codes, int64_t ldc,
                 int words, float* __restrict__ scales) {
   overlap_sync();
   constexpr int W = Vec16<T>::N;
-  extern __shared__ __align__(16) uint8_t staged[];
-  __shared__ RowShared sh;
+  extern __shared__ __align__(16) uint8_t smem[];        // FRAME: codes
+  __shared__ RowShared sh[2];
   const Place at(threads);
-  const bool in = at.row < M;              // lanes of a row past the last still take part in the warp's exchanges
-  const T* xr = x + (in ? at.row : 0) * d;
-  const Span<T, FRAME> f(xr, d);
-  const int v1 = in ? f.v1 : 0, edges = in ? f.edges : 0;
-  Vec16<T> r[NV];
-  uint32_t top = 0u;
+  Feed<T, FRAME, 1, false> feed(0, smem);
+  feed.array(0, x);
+  uint8_t* mine = smem + (size_t)at.group * code_bytes<T>(at.n);
+  Walk w(at);
+  feed.start(w.row, M, d, at);
+  for (int flip = 0; w.lead < M; w.row += w.step, w.lead += w.step, flip ^= 1) {
+    const bool in = w.row < M;             // lanes of a row past the last still take part in the warp's exchanges
+    const T* xr = x + (in ? w.row : 0) * d;
+    const Span<T, FRAME> f(xr, d);
+    const int v1 = in ? f.v1 : 0;
+    const bool has_edge = FRAME && in && at.t < f.edges;
+    feed.begin(w.row, w.row + w.step, M, d, at);
+    float top = 0.f;
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) r[k].load(xr + f.column(v));
-  }
-  auto edge = [&](int c) { return factor ? __fmul_rn(to_f<T>(xr[c]), factor[c]) : to_f<T>(xr[c]); };
-  if constexpr (FRAME) {
-    for (int e = at.t; e < edges; e += at.n) top = max(top, abs_bits(edge(f.edge(e))));
-  }
+    for (int k = 0; k < NV; ++k) {
+      const int v = f.v0 + k * at.n + at.t;
+      if (v < v1) {
+        const Pairs<T> o = scaled<T, FRAME>(feed.raw[0][k], factor, f, v);
 #pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) {
-      float o[W];
-      scaled<T, FRAME>(o, r[k], factor, f, v);
-#pragma unroll
-      for (int i = 0; i < W; ++i) top = max(top, abs_bits(o[i]));
+        for (int i = 0; i < W / 2; ++i) top = max_abs(top, o.v[i]);
+      }
     }
-  }
-  reduce_row<0, true>(nullptr, top, at, &sh);
-  const RowScale rs = row_scale(top, 1.0f);
-  if (at.t == 0 && in) scales[at.row] = rs.scale;
-  int8_t* cr = codes + at.row * ldc;
-  uint8_t* mine = FRAME ? staged + (size_t)at.group * code_bytes<T>(at.n) : nullptr;
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) {
-      float o[W];
-      uint32_t w[W / 4];
-      scaled<T, FRAME>(o, r[k], factor, f, v);
-      code_words<W>(w, o, rs.inv, rs.live);
-      store_words<W>(FRAME ? (void*)(mine + v * W) : (void*)(cr + v * W), w);
+    float ev = 0.f;
+    if (has_edge) {
+      ev = to_f<T>(feed.edge[0]);
+      if (factor) ev = __fmul_rn(ev, factor[f.edge(at.t)]);
+      top = max_abs(top, ev);
     }
-  }
-  if constexpr (FRAME) {
-    for (int e = at.t; e < edges; e += at.n) mine[f.s + f.edge(e)] = one_code(edge(f.edge(e)), rs);
-    codes_out(mine, cr, f.s, in ? d : 0, at, words != 0);
+    reduce_row<0, true>(nullptr, top, at, &sh[flip]);
+    const RowScale rs = row_scale(top, 1.0f);
+    if (at.t == 0 && in) scales[w.row] = rs.scale;
+    int8_t* cr = codes + w.row * ldc;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = f.v0 + k * at.n + at.t;
+      if (v < v1) {
+        uint32_t q[W / 4];
+        code_words<T>(q, scaled<T, FRAME>(feed.raw[0][k], factor, f, v), rs.inv, rs.live);
+        store_words<W>(FRAME ? (void*)(mine + v * W) : (void*)(cr + v * W), q);
+      }
+    }
+    if constexpr (FRAME) {
+      if (has_edge) mine[f.s + f.edge(at.t)] = one_code(ev, rs);
+      codes_out(mine, cr, f.s, in ? d : 0, at, words != 0);
+    }
+    feed.end(w.row + w.step, M, d, at);
   }
 }
 
 // Rows wider than the registers of 1024 threads hold: read twice, the second time from L2.
-template <typename T, bool FRAME>
+template <typename T, int FRAME>
 __global__ void __launch_bounds__(1024)
 quantize_wide_kernel(const T* __restrict__ x, const float* __restrict__ factor, int d, int8_t* __restrict__ codes, int64_t ldc, float* __restrict__ scales) {
   overlap_sync();
@@ -260,15 +410,14 @@ quantize_wide_kernel(const T* __restrict__ x, const float* __restrict__ factor, 
   int8_t* cr = codes + at.row * ldc;
   const Span<T, FRAME> f(xr, d);
   auto edge = [&](int c) { return factor ? __fmul_rn(to_f<T>(xr[c]), factor[c]) : to_f<T>(xr[c]); };
-  uint32_t top = 0u;
-  for (int e = at.t; e < f.edges; e += 1024) top = max(top, abs_bits(edge(f.edge(e))));
+  float top = 0.f;
+  for (int e = at.t; e < f.edges; e += 1024) top = max_abs(top, edge(f.edge(e)));
   for (int v = f.v0 + at.t; v < f.v1; v += 1024) {
     Vec16<T> r;
-    float o[W];
     r.load(xr + f.column(v));
-    scaled<T, FRAME>(o, r, factor, f, v);
+    const Pairs<T> o = scaled<T, FRAME>(r, factor, f, v);
 #pragma unroll
-    for (int i = 0; i < W; ++i) top = max(top, abs_bits(o[i]));
+    for (int i = 0; i < W / 2; ++i) top = max_abs(top, o.v[i]);
   }
   reduce_row<0, true>(nullptr, top, at, &sh);
   const RowScale rs = row_scale(top, 1.0f);
@@ -276,11 +425,9 @@ quantize_wide_kernel(const T* __restrict__ x, const float* __restrict__ factor, 
   for (int e = at.t; e < f.edges; e += 1024) cr[f.edge(e)] = (int8_t)one_code(edge(f.edge(e)), rs);
   for (int v = f.v0 + at.t; v < f.v1; v += 1024) {
     Vec16<T> r;
-    float o[W];
     uint32_t w[W / 4];
     r.load(xr + f.column(v));
-    scaled<T, FRAME>(o, r, factor, f, v);
-    code_words<W>(w, o, rs.inv, rs.live);
+    code_words<T>(w, scaled<T, FRAME>(r, factor, f, v), rs.inv, rs.live);
     if constexpr (!FRAME) store_words<W>(cr + v * W, w);
     else {
 #pragma unroll
@@ -289,7 +436,7 @@ quantize_wide_kernel(const T* __restrict__ x, const float* __restrict__ factor, 
   }
 }
 
-template <typename T, bool FRAME>
+template <typename T, int FRAME>
 __global__ void __launch_bounds__(1024)
 dequantize_kernel(const int8_t* __restrict__ codes, int64_t ldc, const float* __restrict__ scales, int64_t M, int d, int threads, T* __restrict__ y) {
   overlap_sync();
@@ -334,273 +481,273 @@ dequantize_kernel(const int8_t* __restrict__ codes, int64_t ldc, const float* __
     for (int k = 0; k < NV; ++k) {
       const int v = first + k * at.n;
       if (v >= f.v1) continue;
-      float o[W];
+      Pairs<T> o;
 #pragma unroll
-      for (int i = 0; i < W; ++i) o[i] = __fmul_rn((float)(int8_t)(w[k][i / 4] >> (8 * (i & 3))), s);
+      for (int i = 0; i < W; i += 2)
+        o.v[i / 2] = mul2(pack2((float)(int8_t)(w[k][i / 4] >> (8 * (i & 3))), (float)(int8_t)(w[k][i / 4] >> (8 * (i & 3) + 8))), pack2(s, s));
       store_row<T, FRAME>(yr, f, v, true, o);
     }
   }
 }
 
-template <typename T, bool FRAME>
+template <typename T, int FRAME, bool RES>
 __global__ void __launch_bounds__(1024)
 rmsnorm_quantize_kernel(const T* __restrict__ x, const T* __restrict__ resid, const T* __restrict__ g, int64_t M, int d, int threads, float eps,
                         T* __restrict__ h, T* __restrict__ y, int8_t* __restrict__ codes, int64_t ldc, int words, float* __restrict__ scales) {
   overlap_sync();
   constexpr int W = Vec16<T>::N;
-  extern __shared__ __align__(16) uint8_t staged[];
-  __shared__ RowShared sh;
-  const Place at(threads);
-  const bool in = at.row < M;
-  const int64_t row0 = (in ? at.row : 0) * d;
-  const T* xr = x + row0;
-  const T* rr = resid ? resid + row0 : nullptr;
-  const Span<T, FRAME> f(xr, d);
-  const int v1 = in ? f.v1 : 0, edges = in ? f.edges : 0;
-  const bool fit_r = f.fits(rr), fit_h = f.fits(h + row0), fit_y = f.fits(y + row0);
-  // every load of the row before the first use
-  Vec16<T> xv[NV], rv[NV];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) {
-      xv[k].load(xr + f.column(v));
-      if (resid) load_row<T, FRAME>(rv[k], rr, f, v, fit_r);
-    }
-  }
-  float sum = 0.f;
-  uint32_t top = 0u;
-  auto edge = [&](int c) { return resid ? __fadd_rn(to_f<T>(xr[c]), to_f<T>(rr[c])) : to_f<T>(xr[c]); };
-  if constexpr (FRAME) {
-    for (int e = at.t; e < edges; e += at.n) {
-      const float t = edge(f.edge(e));
-      sum = fmaf(t, t, sum);
-      top = max(top, abs_bits(__fmul_rn(t, to_f<T>(g[f.edge(e)]))));
-    }
-  }
-  float o[NV][W];                          // s g: all that the outputs but h need
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) {
-      Vec16<T> gv;
-      load_gain<T, FRAME>(gv, g, f, v);
-      float s[W];
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        s[i] = resid ? __fadd_rn(xv[k].get(i), rv[k].get(i)) : xv[k].get(i);
-        sum = fmaf(s[i], s[i], sum);
-        o[k][i] = __fmul_rn(s[i], gv.get(i));
-        top = max(top, abs_bits(o[k][i]));
-      }
-      if (h) store_row<T, FRAME>(h + row0, f, v, fit_h, s);
-    }
-  }
-  reduce_row<1, true>(&sum, top, at, &sh);
-  const float rstd = rsqrtf(sum / d + eps);
-  const RowScale rs = row_scale(top, rstd);
-  if (at.t == 0 && in) scales[at.row] = rs.scale;
-  int8_t* cr = codes + at.row * ldc;
-  uint8_t* mine = FRAME ? staged + (size_t)at.group * code_bytes<T>(at.n) : nullptr;
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) {
-      uint32_t w[W / 4];
-      code_words<W>(w, o[k], rs.inv, rs.live);
-      store_words<W>(FRAME ? (void*)(mine + v * W) : (void*)(cr + v * W), w);
-      if (y) {
-#pragma unroll
-        for (int i = 0; i < W; ++i) o[k][i] *= rstd;
-        store_row<T, FRAME>(y + row0, f, v, fit_y, o[k]);
-      }
-    }
-  }
-  if constexpr (FRAME) {
-    for (int e = at.t; e < edges; e += at.n) {           // read again: h, which may be x or residual, is written here only
-      const int c = f.edge(e);
-      const float s = edge(c), v = __fmul_rn(s, to_f<T>(g[c]));
-      mine[f.s + c] = one_code(v, rs);
-      if (h) h[row0 + c] = from_f<T>(s);
-      if (y) y[row0 + c] = from_f<T>(v * rstd);
-    }
-    codes_out(mine, cr, f.s, in ? d : 0, at, words != 0);
-  }
-}
-
-// The gradient of one row whose vectors are in registers; acc, acc_edge (DG): this thread's columns of the gain's gradient (DG: a
-// thread has one edge at most).  Contractions are spelled out: dx does not depend on whether dg is asked for.
-template <typename T, bool FRAME, bool DG>
-__device__ __forceinline__ void norm_row_bwd(const Vec16<T>* hv, const Vec16<T>* dv, const Vec16<T>* rv, const T* g, const T* hr, const T* dr, const T* rr,
-                                             const Span<T, FRAME>& f, int v1, int edges, const Place& at, RowShared* sh, float eps, T* dx,
-                                             bool fit_dx, float (*acc)[Vec16<T>::N], float* acc_edge) {
-  constexpr int W = Vec16<T>::N;
-  float s[2] = {0.f, 0.f};
-  if constexpr (FRAME) {
-    for (int e = at.t; e < edges; e += at.n) {
-      const int c = f.edge(e);
-      const float hh = to_f<T>(hr[c]);
-      s[0] = fmaf(hh, hh, s[0]);
-      s[1] = fmaf(__fmul_rn(to_f<T>(dr[c]), to_f<T>(g[c])), hh, s[1]);
-    }
-  }
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) {
-      Vec16<T> gv;
-      load_gain<T, FRAME>(gv, g, f, v);
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float hh = hv[k].get(i);
-        s[0] = fmaf(hh, hh, s[0]);
-        s[1] = fmaf(__fmul_rn(dv[k].get(i), gv.get(i)), hh, s[1]);
-      }
-    }
-  }
-  uint32_t none = 0u;
-  reduce_row<2, false>(s, none, at, sh);
-  const float rstd = rsqrtf(s[0] / f.d + eps);
-  const float c = rstd * rstd * (s[1] / f.d);
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) {
-      Vec16<T> gv;
-      load_gain<T, FRAME>(gv, g, f, v);
-      float o[W];
-#pragma unroll
-      for (int i = 0; i < W; ++i) {
-        const float hh = hv[k].get(i), dd = dv[k].get(i);
-        const float t = fmaf(-hh, c, __fmul_rn(dd, gv.get(i)));
-        o[i] = rr ? fmaf(rstd, t, rv[k].get(i)) : __fmul_rn(rstd, t);
-        if constexpr (DG) acc[k][i] = fmaf(dd, __fmul_rn(hh, rstd), acc[k][i]);
-      }
-      store_row<T, FRAME>(dx, f, v, fit_dx, o);
-    }
-  }
-  if constexpr (FRAME)
-    for (int e = at.t; e < edges; e += at.n) {           // read again: dx, which may be dy or residual, is written here only
-      const int q = f.edge(e);
-      const float hh = to_f<T>(hr[q]), dd = to_f<T>(dr[q]);
-      const float t = fmaf(-hh, c, __fmul_rn(dd, to_f<T>(g[q])));
-      dx[q] = from_f<T>(rr ? fmaf(rstd, t, to_f<T>(rr[q])) : __fmul_rn(rstd, t));
-      if constexpr (DG) *acc_edge = fmaf(dd, __fmul_rn(hh, rstd), *acc_edge);
-    }
-}
-
-template <typename T, bool FRAME>
-__global__ void __launch_bounds__(1024)
-rmsnorm_bwd_kernel(const T* __restrict__ dy, const T* __restrict__ h, const T* __restrict__ g, const T* __restrict__ resid, int64_t M, int d, int threads,
-                   float eps, T* __restrict__ dx) {
-  overlap_sync();
-  __shared__ RowShared sh;
-  const Place at(threads);
-  const bool in = at.row < M;
-  const int64_t row0 = (in ? at.row : 0) * d;
-  const T *hr = h + row0, *dr = dy + row0, *rr = resid ? resid + row0 : nullptr;
-  const Span<T, FRAME> f(hr, d);
-  const int v1 = in ? f.v1 : 0;
-  const bool fit_d = f.fits(dr), fit_r = f.fits(rr);
-  Vec16<T> hv[NV], dv[NV], rv[NV];
-#pragma unroll
-  for (int k = 0; k < NV; ++k) {
-    const int v = f.v0 + k * at.n + at.t;
-    if (v < v1) {
-      hv[k].load(hr + f.column(v));
-      load_row<T, FRAME>(dv[k], dr, f, v, fit_d);
-      if (rr) load_row<T, FRAME>(rv[k], rr, f, v, fit_r);
-    }
-  }
-  norm_row_bwd<T, FRAME, false>(hv, dv, rv, g, hr, dr, rr, f, v1, in ? f.edges : 0, at, &sh, eps, dx + row0, f.fits(dx + row0), nullptr, nullptr);
-}
-
-// With the gain's gradient: the blocks walk the rows, each group of threads every (groups of the grid)-th one, and keep their
-// columns' sums in registers; the groups of a block add theirs up in order, and each block leaves one row of partial
-// sums [gridDim.x, d] that dg_reduce_kernel adds up in order: the result does not depend on scheduling.  A group with more than one
-// row has a stride of a multiple of 8 rows, so its rows all have the same shift.
-// MAXT 512: a thread copies its share of the next row into shared memory while it works on this one; rows that need more threads
-// leave no room for that.
-template <typename T, bool FRAME, int MAXT>
-__global__ void __launch_bounds__(MAXT, 1)
-rmsnorm_bwd_gain_kernel(const T* __restrict__ dy, const T* __restrict__ h, const T* __restrict__ g, const T* __restrict__ resid, int64_t M, int d,
-                        int threads, float eps, T* __restrict__ dx, float* __restrict__ partial) {
-  overlap_sync();
-  constexpr int W = Vec16<T>::N;
-  constexpr bool AHEAD = MAXT <= 512;
-  extern __shared__ __align__(16) uint8_t staged[];      // AHEAD: [2][array][k][thread] vectors of 16 bytes; in the end sums
+  extern __shared__ __align__(16) uint8_t smem[];        // FRAME: codes
   __shared__ RowShared sh[2];
   const Place at(threads);
-  const int per = blockDim.x / threads;
-  const int64_t groups = (int64_t)gridDim.x * per;
-  const int narr = resid ? 3 : 2;
-  const Span<T, FRAME> f(h + at.row * d, d);
-  const bool fit_d = f.fits(dy + at.row * d), fit_r = f.fits(resid + at.row * d), fit_dx = f.fits(dx + at.row * d);
-  auto slot = [&](int stage, int a, int k) { return staged + ((size_t)((stage * narr + a) * NV + k) * blockDim.x + threadIdx.x) * 16; };
-  auto fetch = [&](int64_t row, int stage) {
-    if (AHEAD && row < M) {
+  Feed<T, FRAME, RES ? 2 : 1, false> feed(0, smem);
+  feed.array(0, x);
+  if constexpr (RES) feed.array(1, resid);
+  uint8_t* mine = smem + (size_t)at.group * code_bytes<T>(at.n);
+  const bool fit_h = ((reinterpret_cast<uintptr_t>(h) - reinterpret_cast<uintptr_t>(x)) & 15u) == 0;
+  const bool fit_y = ((reinterpret_cast<uintptr_t>(y) - reinterpret_cast<uintptr_t>(x)) & 15u) == 0;
+  Walk w(at);
+  feed.start(w.row, M, d, at);
+  for (int flip = 0; w.lead < M; w.row += w.step, w.lead += w.step, flip ^= 1) {
+    const bool in = w.row < M;
+    const int64_t row0 = (in ? w.row : 0) * d;
+    const Span<T, FRAME> f(x + row0, d);
+    const int v1 = in ? f.v1 : 0, ec = f.edge(at.t);
+    const bool has_edge = FRAME && in && at.t < f.edges;
+    feed.begin(w.row, w.row + w.step, M, d, at);
+    uint64_t sum2 = 0ull;
+    float es = 0.f, ev = 0.f, top = 0.f;
+    // x + residual, from the vectors as they came: formed twice, which costs less than the registers that would keep it
+    auto sum_of = [&](int k) {
+      Pairs<T> s = pairs_of(feed.raw[0][k]);
+      if constexpr (RES) {
+        const Pairs<T> rp = pairs_of(feed.raw[1][k]);
 #pragma unroll
-      for (int a = 0; a < 3; ++a) {
-        if ((a == 1 && !fit_d) || (a == 2 && (!resid || !fit_r))) continue;
-        const T* p = (a == 0 ? h : a == 1 ? dy : resid) + row * d;
+        for (int i = 0; i < W / 2; ++i) s.v[i] = add2(s.v[i], rp.v[i]);
+      }
+      return s;
+    };
 #pragma unroll
-        for (int k = 0; k < NV; ++k) {
-          const int v = f.v0 + k * at.n + at.t;
-          if (v < f.v1)
-            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(slot(stage, a, k))), "l"(p + f.column(v)) : "memory");
+    for (int k = 0; k < NV; ++k) {
+      const int v = f.v0 + k * at.n + at.t;
+      if (v < v1) {
+        Vec16<T> gv;
+        load_gain<T, FRAME>(gv, g, f, v);
+        const Pairs<T> s = sum_of(k), gain = pairs_of(gv);
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) {
+          sum2 = fma2(s.v[i], s.v[i], sum2);
+          top = max_abs(top, mul2(s.v[i], gain.v[i]));
+        }
+        if (h) store_row<T, FRAME>(h + row0, f, v, fit_h, s);
+      }
+    }
+    float sum;
+    {
+      float a, b;
+      unpack2(sum2, a, b);
+      sum = a + b;
+    }
+    if (has_edge) {
+      es = to_f<T>(feed.edge[0]);
+      if constexpr (RES) es = __fadd_rn(es, to_f<T>(feed.edge[1]));
+      ev = __fmul_rn(es, to_f<T>(g[ec]));
+      sum = fmaf(es, es, sum);
+      top = max_abs(top, ev);
+      if (h) h[row0 + ec] = from_f<T>(es);
+    }
+    reduce_row<1, true>(&sum, top, at, &sh[flip]);
+    const float rstd = rsqrtf(sum / d + eps);
+    const RowScale rs = row_scale(top, rstd);
+    if (at.t == 0 && in) scales[w.row] = rs.scale;
+    int8_t* cr = codes + w.row * ldc;
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = f.v0 + k * at.n + at.t;
+      if (v < v1) {
+        Vec16<T> gv;
+        load_gain<T, FRAME>(gv, g, f, v);
+        Pairs<T> o = sum_of(k);
+        const Pairs<T> gain = pairs_of(gv);
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) o.v[i] = mul2(o.v[i], gain.v[i]);
+        uint32_t q[W / 4];
+        code_words<T>(q, o, rs.inv, rs.live);
+        store_words<W>(FRAME ? (void*)(mine + v * W) : (void*)(cr + v * W), q);
+        if (y) {
+          const uint64_t rstd2 = pack2(rstd, rstd);
+#pragma unroll
+          for (int i = 0; i < W / 2; ++i) o.v[i] = mul2(o.v[i], rstd2);
+          store_row<T, FRAME>(y + row0, f, v, fit_y, o);
         }
       }
     }
-    asm volatile("cp.async.commit_group;" ::: "memory");
-  };
-  auto take = [&](Vec16<T>& r, int stage, int a, int k, const T* p, bool fits) {
-    if (AHEAD && fits) r.raw = *reinterpret_cast<const decltype(r.raw)*>(slot(stage, a, k));
-    else load_row<T, FRAME>(r, p, f, f.v0 + k * at.n + at.t, fits);
-  };
-  float acc[NV][W], acc_edge = 0.f;
+    if constexpr (FRAME) {
+      if (has_edge) {
+        mine[f.s + ec] = one_code(ev, rs);
+        if (y) y[row0 + ec] = from_f<T>(ev * rstd);
+      }
+      codes_out(mine, cr, f.s, in ? d : 0, at, words != 0);
+    }
+    feed.end(w.row + w.step, M, d, at);
+  }
+}
+
+// The gradient.  Contractions are spelled out: dx does not depend on whether dg is asked for.
+// DG: the gain's gradient too.  A group keeps its columns' sums in registers; the groups of a block add theirs up in order, and each
+// block leaves one row of partial sums [gridDim.x, d] that dg_reduce_kernel adds up in order: the result does not depend on
+// scheduling.  The number of groups is then a multiple of 8 (or each has one row), so a group's rows all have the same shift and
+// its threads the same columns.
+template <typename T, int FRAME, bool DG, bool RES, int MAXT>
+__global__ void __launch_bounds__(MAXT)
+rmsnorm_bwd_kernel(const T* __restrict__ dy, const T* __restrict__ h, const T* __restrict__ g, const T* __restrict__ resid, int64_t M, int d, int threads,
+                   int stages, float eps, T* __restrict__ dx, float* __restrict__ partial) {
+  overlap_sync();
+  constexpr int W = Vec16<T>::N;
+  extern __shared__ __align__(16) uint8_t smem[];        // the feed's slots; in the end (DG) sums
+  __shared__ RowShared sh[2];
+  const Place at(threads);
+  Feed<T, FRAME, RES ? 3 : 2, DG, 2> feed(stages, smem);
+  feed.array(0, h);
+  feed.array(1, dy);
+  if constexpr (RES) feed.array(2, resid);
+  const bool fit_dx = ((reinterpret_cast<uintptr_t>(dx) - reinterpret_cast<uintptr_t>(h)) & 15u) == 0;
+  Pairs<T> acc[DG ? NV : 1];
+  float acc_edge = 0.f;
+  if constexpr (DG) {
 #pragma unroll
-  for (int k = 0; k < NV; ++k)
+    for (int k = 0; k < NV; ++k)
 #pragma unroll
-    for (int i = 0; i < W; ++i) acc[k][i] = 0.f;
-  fetch(at.row, 0);
-  int stage = 0;
-  // every thread of the block goes through the same number of rows
-  for (int64_t row = at.row, lead = (int64_t)blockIdx.x * per; lead < M; row += groups, lead += groups, stage ^= 1) {
-    const bool in = row < M;
-    const int64_t row0 = (in ? row : 0) * d;
-    const T *hr = h + row0, *dr = dy + row0, *rr = resid ? resid + row0 : nullptr;
-    Vec16<T> hv[NV], dv[NV], rv[NV];
-    fetch(row + groups, stage ^ 1);
-    asm volatile("cp.async.wait_group 1;" ::: "memory");
+      for (int i = 0; i < W / 2; ++i) acc[k].v[i] = 0ull;
+  }
+  Walk w(at);
+  const Span<T, FRAME> own(h + w.row * d, d);            // of all rows of this group (DG)
+  feed.start(w.row, M, d, at);
+  for (int flip = 0; w.lead < M; w.row += w.step, w.lead += w.step, flip ^= 1) {
+    const bool in = w.row < M;
+    const int64_t row0 = (in ? w.row : 0) * d;
+    const Span<T, FRAME> f(h + row0, d);
+    const int v1 = in ? f.v1 : 0, ec = f.edge(at.t);
+    const bool has_edge = FRAME && in && at.t < f.edges;
+    feed.begin(w.row, w.row + w.step, M, d, at);
+    Vec16<T> kept[2][DG ? NV : 1];          // AHEAD: out of the slots, once
+    auto vec = [&](int a, int k) -> const Vec16<T>& { if constexpr (DG) return kept[a][k]; else return feed.raw[a][k]; };
+    uint64_t hh2 = 0ull, wh2 = 0ull;
+    float eh = 0.f, ed = 0.f, eg = 0.f;
 #pragma unroll
     for (int k = 0; k < NV; ++k) {
-      if (in && f.v0 + k * at.n + at.t < f.v1) {
-        take(hv[k], stage, 0, k, hr, true);
-        take(dv[k], stage, 1, k, dr, fit_d);
-        if (rr) take(rv[k], stage, 2, k, rr, fit_r);
+      const int v = f.v0 + k * at.n + at.t;
+      if (v < v1) {
+        Vec16<T> gv;
+        if constexpr (DG) {
+          feed.take(kept[0][k], 0, k, h + row0, f.column(v));
+          feed.take(kept[1][k], 1, k, dy + row0, f.column(v));
+        }
+        load_gain<T, FRAME>(gv, g, f, v);
+        const Pairs<T> hp = pairs_of(vec(0, k)), dp = pairs_of(vec(1, k)), gp = pairs_of(gv);
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) {
+          hh2 = fma2(hp.v[i], hp.v[i], hh2);
+          wh2 = fma2(mul2(dp.v[i], gp.v[i]), hp.v[i], wh2);
+        }
       }
     }
-    norm_row_bwd<T, FRAME, true>(hv, dv, rv, g, hr, dr, rr, f, in ? f.v1 : 0, in ? f.edges : 0, at, &sh[stage], eps, dx + row0, fit_dx, acc, &acc_edge);
-  }
-  asm volatile("cp.async.wait_group 0;" ::: "memory");
-  __syncthreads();
-  float* sums = reinterpret_cast<float*>(staged);
-  for (int c = threadIdx.x; c < d; c += blockDim.x) sums[c] = 0.f;
-  __syncthreads();
-  for (int gr = 0; gr < per; ++gr) {
-    if (at.group == gr) {
+    float s[2];
+    {
+      float a, b;
+      unpack2(hh2, a, b); s[0] = a + b;
+      unpack2(wh2, a, b); s[1] = a + b;
+    }
+    if (has_edge) {
+      eh = to_f<T>(feed.edge[0]); ed = to_f<T>(feed.edge[1]); eg = to_f<T>(g[ec]);
+      s[0] = fmaf(eh, eh, s[0]);
+      s[1] = fmaf(__fmul_rn(ed, eg), eh, s[1]);
+    }
+    // the residual's vectors: under way during the reduction, where registers are free for them (not with edges or sums to keep)
+    constexpr bool SOON = RES && !DG && FRAME == FRAME_NONE;
+    Vec16<T> rv[SOON ? NV : 1];
+    if constexpr (SOON) {
 #pragma unroll
       for (int k = 0; k < NV; ++k) {
         const int v = f.v0 + k * at.n + at.t;
-#pragma unroll
-        for (int i = 0; i < W; ++i) if (v < f.v1) sums[f.column(v) + i] += acc[k][i];
+        if (v < v1) rv[k].load(resid + row0 + f.column(v));
       }
-      if (FRAME && at.t < f.edges) sums[f.edge(at.t)] += acc_edge;
     }
-    __syncthreads();
+    float none = 0.f;
+    reduce_row<2, false>(s, none, at, &sh[flip]);
+    const float rstd = rsqrtf(s[0] / d + eps);
+    const float c = rstd * rstd * (s[1] / d);
+    const uint64_t rstd2 = pack2(rstd, rstd), c2 = pack2(-c, -c);
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+      const int v = f.v0 + k * at.n + at.t;
+      if (v < v1) {
+        Vec16<T> gv;
+        load_gain<T, FRAME>(gv, g, f, v);
+        const Pairs<T> hp = pairs_of(vec(0, k)), dp = pairs_of(vec(1, k)), gp = pairs_of(gv);
+        Pairs<T> o;
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) o.v[i] = fma2(hp.v[i], c2, mul2(dp.v[i], gp.v[i]));
+        if constexpr (RES) {
+          if constexpr (DG) feed.take(rv[0], 2, k, resid + row0, f.column(v));
+          else if constexpr (!SOON) feed.read(rv[0], 2, resid + row0 + f.column(v));
+          const Pairs<T> rp = pairs_of(rv[SOON ? k : 0]);
+#pragma unroll
+          for (int i = 0; i < W / 2; ++i) o.v[i] = fma2(rstd2, o.v[i], rp.v[i]);
+        } else {
+#pragma unroll
+          for (int i = 0; i < W / 2; ++i) o.v[i] = mul2(rstd2, o.v[i]);
+        }
+        if constexpr (DG) {
+#pragma unroll
+          for (int i = 0; i < W / 2; ++i) acc[k].v[i] = fma2(dp.v[i], mul2(hp.v[i], rstd2), acc[k].v[i]);
+        }
+        store_row<T, FRAME>(dx + row0, f, v, fit_dx, o);
+      }
+    }
+    if (has_edge) {
+      const float t = fmaf(-eh, c, __fmul_rn(ed, eg));
+      if constexpr (RES) dx[row0 + ec] = from_f<T>(fmaf(rstd, t, to_f<T>(feed.edge[2])));
+      else dx[row0 + ec] = from_f<T>(__fmul_rn(rstd, t));
+      if constexpr (DG) acc_edge = fmaf(ed, __fmul_rn(eh, rstd), acc_edge);
+    }
+    feed.end(w.row + w.step, M, d, at);
   }
-  float* out = partial + (int64_t)blockIdx.x * d;
-  for (int c = threadIdx.x; c < d; c += blockDim.x) out[c] = sums[c];
+  feed.finish();
+  if constexpr (DG) {
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(smem);
+    for (int c = threadIdx.x; c < d; c += blockDim.x) sums[c] = 0.f;
+    __syncthreads();
+    // several rows per warp with the same columns per lane: added up in the warp first, which then takes one turn
+    const int lane = threadIdx.x & 31, mates = FRAME == FRAME_NONE && at.n < 32 ? 32 / at.n : 1;
+    for (int o = at.n; o < at.n * mates; o <<= 1) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k)
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) acc[k].v[i] = add2(acc[k].v[i], __shfl_xor_sync(0xffffffffu, acc[k].v[i], o));
+    }
+    for (int turn = 0; turn < (int)blockDim.x / (threads * mates); ++turn) {
+      if (at.group / mates == turn && (mates == 1 || lane < at.n)) {
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+          const int v = own.v0 + k * at.n + at.t;
+          if (v < own.v1) {
+#pragma unroll
+            for (int i = 0; i < W / 2; ++i) {
+              float a, b;
+              unpack2(acc[k].v[i], a, b);
+              sums[own.column(v) + 2 * i] += a;
+              sums[own.column(v) + 2 * i + 1] += b;
+            }
+          }
+        }
+        if (FRAME && at.t < own.edges) sums[own.edge(at.t)] += acc_edge;
+      }
+      __syncthreads();
+    }
+    float* out = partial + (int64_t)blockIdx.x * d;
+    for (int c = threadIdx.x; c < d; c += blockDim.x) out[c] = sums[c];
+  }
 }
 
 // 32 columns per block, 8 threads per column, each adding every eighth partial row in order.
@@ -623,24 +770,72 @@ __global__ void __launch_bounds__(256) dg_reduce_kernel(const float* __restrict_
 
 bool al(const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(a - 1)) == 0; }
 
-// Threads per row: as many as give each NV accesses, a power of two up to a warp, else whole warps; at least `least`.
-template <typename T> int row_threads(int d, int least = 1) {
+// Threads per row: as many as give each NV accesses, a power of two up to a warp, else whole warps.  frame: an edge per thread.
+template <typename T> int row_threads(int d, bool frame) {
   const int nv = (d + Vec16<T>::N - 1) / Vec16<T>::N, need = (nv + NV - 1) / NV;
   if (need > 32) return (need + 31) / 32 * 32;
-  int n = least;
+  int n = frame ? 2 * Vec16<T>::N : 1;
   while (n < need) n *= 2;
   return n;
 }
+
 // Blocks of 256 threads where a row takes a warp or less, else a block per row.
-struct Shape { int threads, block; int64_t blocks; };
+struct Shape { int block, per; int64_t blocks; };
 Shape shape_of(int64_t M, int threads) {
   Shape s;
-  s.threads = threads;
   s.block = threads <= 32 ? 256 : threads;
-  const int per = s.block / threads;
-  s.blocks = (M + per - 1) / per;
+  s.per = s.block / threads;
+  s.blocks = (M + s.per - 1) / s.per;
   return s;
 }
+
+template <typename T, int FRAME>
+cudaError_t quantize_t(const T* x, const float* factor, int64_t M, int d, int threads, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+  const Shape s = shape_of(M, threads);
+  const int words = ldc % 4 == 0 && al(codes, 4);
+  return launch_overlapped(quantize_kernel<T, FRAME>, dim3((unsigned)s.blocks), dim3(s.block), FRAME ? (size_t)s.per * code_bytes<T>(threads) : 0, st, x, factor,
+                           M, d, threads, codes, ldc, words, scales);
+}
+template <typename T, int FRAME>
+cudaError_t norm_t(const T* x, const T* resid, const T* g, int64_t M, int d, float eps, T* h, T* y, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+  const int threads = row_threads<T>(d, FRAME != 0);
+  const Shape s = shape_of(M, threads);
+  const int words = ldc % 4 == 0 && al(codes, 4);
+  return launch_overlapped(resid ? rmsnorm_quantize_kernel<T, FRAME, true> : rmsnorm_quantize_kernel<T, FRAME, false>, dim3((unsigned)s.blocks), dim3(s.block),
+                           FRAME ? (size_t)s.per * code_bytes<T>(threads) : 0, st, x, resid, g, M, d, threads, eps, h, y, codes, ldc, words, scales);
+}
+template <typename T, int FRAME>
+cudaError_t norm_bwd_t(const T* dy, const T* h, const T* g, const T* resid, int64_t M, int d, int threads, float eps, T* dx, cudaStream_t st) {
+  const Shape s = shape_of(M, threads);
+  return launch_overlapped(resid ? rmsnorm_bwd_kernel<T, FRAME, false, true, 1024> : rmsnorm_bwd_kernel<T, FRAME, false, false, 1024>, dim3((unsigned)s.blocks),
+                           dim3(s.block), 0, st, dy, h, g, resid, M, d, threads, 0, eps, dx, (float*)nullptr);
+}
+// With dg: as many rows per block as 512 threads take, a block per SM (128 registers per thread, up to 192 KB of copies ahead).
+template <typename T, int FRAME, int MAXT>
+cudaError_t norm_gain_t(const T* dy, const T* h, const T* g, const T* resid, int64_t M, int d, int threads, float eps, T* dx, float* partial, int* rows,
+                        cudaStream_t st) {
+  constexpr size_t MOST = 230000;
+  const auto kernel = resid ? rmsnorm_bwd_kernel<T, FRAME, true, true, MAXT> : rmsnorm_bwd_kernel<T, FRAME, true, false, MAXT>;
+  static PerDeviceOnce once[2];
+  const int dev = current_device();
+  if (once[resid ? 1 : 0].needed(dev)) {
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST);
+    if (e != cudaSuccess) return e;
+    once[resid ? 1 : 0].done(dev);
+  }
+  const int per = threads > 512 ? 1 : 512 / threads, block = per * threads;
+  const size_t one = (size_t)(resid ? 3 : 2) * NV * block * 16;
+  const int stages = 2 * one <= MOST ? 2 : 1;
+  const size_t smem = stages * one < (size_t)d * 4 ? (size_t)d * 4 : stages * one;
+  const int64_t all = (M + per - 1) / per;
+  int64_t blocks = num_sms() < DG_PARTIAL_ROWS ? num_sms() : DG_PARTIAL_ROWS;
+  if (blocks >= all) blocks = all;
+  else blocks = blocks >= 8 ? blocks / 8 * 8 : 8;
+  *rows = (int)blocks;
+  return launch_overlapped(kernel, dim3((unsigned)blocks), dim3(block), smem, st, dy, h, g, resid, M, d, threads, stages, eps, dx, partial);
+}
+// Arrays at the same place of a 16-byte vector as the first one.
+bool same_place(const void* p, const void* first) { return !p || ((reinterpret_cast<uintptr_t>(p) - reinterpret_cast<uintptr_t>(first)) & 15u) == 0; }
 
 }  // namespace
 
@@ -649,17 +844,12 @@ cudaError_t quantize_rows(int dt, const void* x, const float* factor, int64_t M,
     using T = decltype(type);
     constexpr int W = Vec16<T>::N;
     const bool frame = d % W != 0 || ldc % W != 0 || !al(x, 16) || !al(factor, 16) || !al(codes, W);
-    const int threads = row_threads<T>(d);
+    const int threads = row_threads<T>(d, frame);
     if (threads > 1024)
-      return frame ? launch_overlapped(quantize_wide_kernel<T, true>, dim3((unsigned)M), dim3(1024), 0, st, (const T*)x, factor, d, codes, ldc, scales)
-                   : launch_overlapped(quantize_wide_kernel<T, false>, dim3((unsigned)M), dim3(1024), 0, st, (const T*)x, factor, d, codes, ldc, scales);
-    const Shape s = shape_of(M, threads);
-    const int words = ldc % 4 == 0 && al(codes, 4);
-    const size_t smem = frame ? (size_t)(s.block / threads) * code_bytes<T>(threads) : 0;
-    auto go = [&](auto kernel) {
-      return launch_overlapped(kernel, dim3((unsigned)s.blocks), dim3(s.block), smem, st, (const T*)x, factor, M, d, threads, codes, ldc, words, scales);
-    };
-    return frame ? go(quantize_kernel<T, true>) : go(quantize_kernel<T, false>);
+      return launch_overlapped(frame ? quantize_wide_kernel<T, FRAME_SAME> : quantize_wide_kernel<T, FRAME_NONE>, dim3((unsigned)M), dim3(1024), 0, st, (const T*)x,
+                               factor, d, codes, ldc, scales);
+    return frame ? quantize_t<T, FRAME_SAME>((const T*)x, factor, M, d, threads, codes, ldc, scales, st)
+                 : quantize_t<T, FRAME_NONE>((const T*)x, factor, M, d, threads, codes, ldc, scales, st);
   };
   return dt == DT_BF16 ? run(bf16()) : run(float());
 }
@@ -669,11 +859,11 @@ cudaError_t dequantize_rows(int dt, const int8_t* codes, int64_t ldc, const floa
     using T = decltype(type);
     constexpr int W = Vec16<T>::N;
     const bool frame = d % W != 0 || ldc % W != 0 || !al(y, 16) || !al(codes, W);
-    int threads = row_threads<T>(d);
+    int threads = row_threads<T>(d, frame);
     if (threads > 1024) threads = 1024;
-    const Shape s = shape_of(M, threads);
-    return launch_overlapped(frame ? dequantize_kernel<T, true> : dequantize_kernel<T, false>, dim3((unsigned)s.blocks), dim3(s.block), 0, st, codes, ldc,
-                             scales, M, d, threads, (T*)y);
+    const int block = threads <= 32 ? 256 : threads, per = block / threads;
+    return launch_overlapped(frame ? dequantize_kernel<T, FRAME_SAME> : dequantize_kernel<T, FRAME_NONE>, dim3((unsigned)((M + per - 1) / per)), dim3(block), 0, st,
+                             codes, ldc, scales, M, d, threads, (T*)y);
   };
   return dt == DT_BF16 ? run(bf16()) : run(float());
 }
@@ -684,39 +874,12 @@ cudaError_t rmsnorm_quantize(int dt, const void* x, const void* resid, const voi
     using T = decltype(type);
     constexpr int W = Vec16<T>::N;
     const bool frame = d % W != 0 || ldc % W != 0 || !al(x, 16) || !al(g, 16) || !al(resid, 16) || !al(h, 16) || !al(y, 16) || !al(codes, W);
-    const int threads = row_threads<T>(d);
-    const Shape s = shape_of(M, threads);
-    const int words = ldc % 4 == 0 && al(codes, 4);
-    const size_t smem = frame ? (size_t)(s.block / threads) * code_bytes<T>(threads) : 0;
-    auto go = [&](auto kernel) {
-      return launch_overlapped(kernel, dim3((unsigned)s.blocks), dim3(s.block), smem, st, (const T*)x, (const T*)resid, (const T*)g, M, d, threads, eps,
-                               (T*)h, (T*)y, codes, ldc, words, scales);
-    };
-    return frame ? go(rmsnorm_quantize_kernel<T, true>) : go(rmsnorm_quantize_kernel<T, false>);
+    auto go = [&](auto launch) { return launch((const T*)x, (const T*)resid, (const T*)g, M, d, eps, (T*)h, (T*)y, codes, ldc, scales, st); };
+    if (!frame) return go(norm_t<T, FRAME_NONE>);
+    return same_place(resid, x) && same_place(h, x) && same_place(y, x) ? go(norm_t<T, FRAME_SAME>) : go(norm_t<T, FRAME_ANY>);
   };
   return dt == DT_BF16 ? run(bf16()) : run(float());
 }
-
-namespace {
-template <typename T, bool FRAME, int MAXT>
-cudaError_t launch_gain(const void* dy, const void* h, const void* g, const void* resid, int64_t M, int d, int threads, int block, int64_t blocks,
-                        float eps, void* dx, float* partial, cudaStream_t st) {
-  constexpr int MOST = MAXT <= 512 ? 2 * 3 * NV * 512 * 16 : ROWS_MAX_WIDTH * 4;
-  static_assert(MOST >= ROWS_MAX_WIDTH * 4 && MOST <= 230000, "");
-  const auto kernel = rmsnorm_bwd_gain_kernel<T, FRAME, MAXT>;
-  static PerDeviceOnce once;
-  const int dev = current_device();
-  if (once.needed(dev)) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, MOST);
-    if (e != cudaSuccess) return e;
-    once.done(dev);
-  }
-  size_t smem = (size_t)d * 4;
-  if constexpr (MAXT <= 512) smem = std::max(smem, (size_t)2 * (resid ? 3 : 2) * NV * block * 16);
-  return launch_overlapped(kernel, dim3((unsigned)blocks), dim3(block), smem, st, (const T*)dy, (const T*)h, (const T*)g,
-                           (const T*)resid, M, d, threads, eps, (T*)dx, partial);
-}
-}  // namespace
 
 size_t rmsnorm_dg_scratch_floats(int64_t M, int d) { return (size_t)(M < DG_PARTIAL_ROWS ? M : DG_PARTIAL_ROWS) * d; }
 
@@ -724,28 +887,22 @@ cudaError_t rmsnorm_gain_bwd(int dt, const void* dy, const void* h, const void* 
                              float* partial, cudaStream_t st) {
   auto run = [&](auto type) -> cudaError_t {
     using T = decltype(type);
-    constexpr int W = Vec16<T>::N;
-    const bool frame = d % W != 0 || !al(dy, 16) || !al(h, 16) || !al(g, 16) || !al(resid, 16) || !al(dx, 16);
-    const int threads = row_threads<T>(d, frame ? 2 * W : 1);       // an edge per thread
+    const bool frame = d % Vec16<T>::N != 0 || !al(dy, 16) || !al(h, 16) || !al(g, 16) || !al(resid, 16) || !al(dx, 16);
+    const int threads = row_threads<T>(d, frame);
+    const bool same = same_place(dy, h) && same_place(resid, h) && same_place(dx, h);
     if (!dg) {
-      const Shape s = shape_of(M, threads);
-      auto go = [&](auto kernel) {
-        return launch_overlapped(kernel, dim3((unsigned)s.blocks), dim3(s.block), 0, st, (const T*)dy, (const T*)h, (const T*)g, (const T*)resid, M, d,
-                                 threads, eps, (T*)dx);
-      };
-        return frame ? go(rmsnorm_bwd_kernel<T, true>) : go(rmsnorm_bwd_kernel<T, false>);
+      auto go = [&](auto launch) { return launch((const T*)dy, (const T*)h, (const T*)g, (const T*)resid, M, d, threads, eps, (T*)dx, st); };
+      if (!frame) return go(norm_bwd_t<T, FRAME_NONE>);
+      return same ? go(norm_bwd_t<T, FRAME_SAME>) : go(norm_bwd_t<T, FRAME_ANY>);
     }
-    const int per = threads > 512 ? 1 : 512 / threads, block = per * threads;
-    int64_t blocks = num_sms() < DG_PARTIAL_ROWS ? num_sms() : DG_PARTIAL_ROWS;
-    if (blocks * per >= M) blocks = (M + per - 1) / per;
-    else if (blocks >= 8) blocks = blocks / 8 * 8;
-    else if (frame) blocks = M < 8 ? M : 8;
-    const cudaError_t e = threads > 512 ? (frame ? launch_gain<T, true, 1024>(dy, h, g, resid, M, d, threads, block, blocks, eps, dx, partial, st)
-                                                 : launch_gain<T, false, 1024>(dy, h, g, resid, M, d, threads, block, blocks, eps, dx, partial, st))
-                                        : (frame ? launch_gain<T, true, 512>(dy, h, g, resid, M, d, threads, block, blocks, eps, dx, partial, st)
-                                                 : launch_gain<T, false, 512>(dy, h, g, resid, M, d, threads, block, blocks, eps, dx, partial, st));
+    int rows = 0;
+    auto go = [&](auto launch) { return launch((const T*)dy, (const T*)h, (const T*)g, (const T*)resid, M, d, threads, eps, (T*)dx, partial, &rows, st); };
+    cudaError_t e = cudaSuccess;
+    if (threads <= 512) e = !frame ? go(norm_gain_t<T, FRAME_NONE, 512>) : same ? go(norm_gain_t<T, FRAME_SAME, 512>) : go(norm_gain_t<T, FRAME_ANY, 512>);
+    else if constexpr (sizeof(T) == 4)
+      e = !frame ? go(norm_gain_t<T, FRAME_NONE, 1024>) : same ? go(norm_gain_t<T, FRAME_SAME, 1024>) : go(norm_gain_t<T, FRAME_ANY, 1024>);
     if (e != cudaSuccess) return e;
-    return launch_overlapped(dg_reduce_kernel, dim3((unsigned)((d + 31) / 32)), dim3(256), 0, st, (const float*)partial, (int)blocks, d, dg);
+    return launch_overlapped(dg_reduce_kernel, dim3((unsigned)((d + 31) / 32)), dim3(256), 0, st, (const float*)partial, rows, d, dg);
   };
   return dt == DT_BF16 ? run(bf16()) : run(float());
 }
