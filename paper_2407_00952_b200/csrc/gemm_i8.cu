@@ -8,6 +8,7 @@
 //                         linear layers (gemm_tc.cu), at twice the operations per byte.
 //   gemm_i8_split_kernel  few tiles: one 128 x 64 tile per cluster of 1-8 CTAs that share the contraction and add their integer
 //                         sums through distributed shared memory.
+//   gemm_i8_rows_kernel   up to 4 tokens: a pass over the weight in plain vector loads and dp4a, a warp per few channels.
 //   gemm_i8_simt_kernel   codes whose rows do not start on 16-byte boundaries (copies cannot take them).
 // Every wait on an mbarrier is bounded; when it expires the kernel records a code in `status` and returns.
 #include "host_common.h"
@@ -26,6 +27,7 @@ constexpr int TILE_BYTES = BM * KB;        // 128 rows
 struct I8Params {
   int M, N, num_kb;
   int tiles_m, tiles_n;
+  int x_rows;                              // rows of x that a copy brings: 128, or as many (of 8) as there are
   const float* sx; const float* sw;        // sw, bias, R may be null
   const void* bias; const void* R; void* Y;
   int* status;
@@ -381,7 +383,8 @@ gemm_i8_split_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_cons
       if (!mbar_wait_warp(empty_bar(stage), phase ^ 1u, abort_flag, p.status, 71)) break;
       const uint32_t sa = base + stage * C::STAGE_BYTES, sb = sa + C::A_BYTES;
       if (leader) {
-        mbar_expect_tx(full_bar(stage), C::STAGE_BYTES);
+        // rows of the x tile past the last token stay as they are: their accumulators are not stored
+        mbar_expect_tx(full_bar(stage), C::B_BYTES + p.x_rows * KB);
         tma_load_2d(sb, &mapW, full_bar(stage), kb * KB, n0);
         tma_load_2d(sa, &mapX, full_bar(stage), kb * KB, m0);
       }
@@ -472,6 +475,69 @@ gemm_i8_split_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_cons
     tc_fence_after();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem_base), "r"((uint32_t)C::BN) : "memory");
   }
+}
+
+// ------------------------------------------------------------------------------------------
+// few tokens
+// ------------------------------------------------------------------------------------------
+// The time of a weight read once: a warp takes C channels (rows of W) and all MR tokens, 512 bytes of a row per step, four codes
+// per dp4a; x comes from L1, C times less often than W from memory.
+template <typename TO, int MR, int C>
+__global__ void __launch_bounds__(256)
+gemm_i8_rows_kernel(const int8_t* __restrict__ x, int64_t ldx, const int8_t* __restrict__ w, int64_t ldw, int K, I8Params p) {
+  overlap_sync();
+  const int lane = threadIdx.x & 31, n0 = ((int)blockIdx.x * 8 + (threadIdx.x >> 5)) * C;
+  if (n0 >= p.N) return;
+  int acc[MR][C];
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int c = 0; c < C; ++c) acc[m][c] = 0;
+  auto row = [&](int c) { return w + (int64_t)min(n0 + c, p.N - 1) * ldw; };
+  auto token = [&](int m) { return x + (int64_t)min(m, p.M - 1) * ldx; };
+  auto add = [&](const uint4 (&b)[C], const uint4& a, int m) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      acc[m][c] = __dp4a((int)a.x, (int)b[c].x, acc[m][c]);
+      acc[m][c] = __dp4a((int)a.y, (int)b[c].y, acc[m][c]);
+      acc[m][c] = __dp4a((int)a.z, (int)b[c].z, acc[m][c]);
+      acc[m][c] = __dp4a((int)a.w, (int)b[c].w, acc[m][c]);
+    }
+  };
+  const int whole = K & ~15;
+  constexpr int U = 8 / C;                 // steps whose weights are under way together
+  for (int k0 = lane * 16; k0 < whole; k0 += 512 * U) {
+    uint4 b[U][C];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + 512 * u < whole) {
+#pragma unroll
+        for (int c = 0; c < C; ++c) b[u][c] = __ldcs(reinterpret_cast<const uint4*>(row(c) + k0 + 512 * u));
+      }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (k0 + 512 * u < whole) {
+#pragma unroll
+        for (int m = 0; m < MR; ++m) add(b[u], *reinterpret_cast<const uint4*>(token(m) + k0 + 512 * u), m);
+      }
+  }
+  if (lane < K - whole) {                  // the last codes one by one: what lies behind a row does not count
+#pragma unroll
+    for (int m = 0; m < MR; ++m)
+#pragma unroll
+      for (int c = 0; c < C; ++c) acc[m][c] += (int)token(m)[whole + lane] * (int)row(c)[whole + lane];
+  }
+#pragma unroll
+  for (int m = 0; m < MR; ++m)
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const int sum = __reduce_add_sync(0xffffffffu, acc[m][c]), n = n0 + c;
+      if (lane != (m * C + c) % 32 || m >= p.M || n >= p.N) continue;
+      const size_t at = (size_t)m * p.N + n;
+      float v = fmaf(__int2float_rn(sum), p.sx[m] * (p.sw ? p.sw[n] : 1.0f), p.bias ? to_f<TO>(reinterpret_cast<const TO*>(p.bias)[n]) : 0.f);
+      if (p.R) v += to_f<TO>(reinterpret_cast<const TO*>(p.R)[at]);
+      reinterpret_cast<TO*>(p.Y)[at] = from_f<TO>(v);
+    }
 }
 
 // ------------------------------------------------------------------------------------------
@@ -610,12 +676,15 @@ Pick pick(const I8Args& a) {
   return best;
 }
 
-template <typename TO, bool VEC> cudaError_t launch_tc(const I8Args& a, const I8Params& p, cudaStream_t st) {
+template <typename TO, bool VEC> cudaError_t launch_tc(const I8Args& a, I8Params p, cudaStream_t st) {
   CUtensorMap mX, mY;
-  if (!map_codes(&mX, a.X, a.M, a.K, a.ldx, BM)) return cudaErrorInvalidValue;
+  const Pick k = pick(a);
+  const bool split = k != PICK_PAIR256 && k != PICK_PAIR128;
+  p.x_rows = split && a.M < BM ? (a.M + 7) / 8 * 8 : BM;
+  if (!map_codes(&mX, a.X, a.M, a.K, a.ldx, (uint32_t)p.x_rows)) return cudaErrorInvalidValue;
   mY = mX;
   if (VEC && !cached_map_2d(&mY, a.Y, a.M, a.N, a.N, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE)) return cudaErrorInvalidValue;
-  switch (pick(a)) {
+  switch (k) {
     case PICK_PAIR256: return launch_pair<TO, VEC, 256>(a, p, mX, mY, st);
     case PICK_PAIR128: return launch_pair<TO, VEC, 128>(a, p, mX, mY, st);
     case PICK_SPLIT2: return launch_split<TO, VEC, 2>(a, p, mX, mY, st);
@@ -623,6 +692,19 @@ template <typename TO, bool VEC> cudaError_t launch_tc(const I8Args& a, const I8
     case PICK_SPLIT8: return launch_split<TO, VEC, 8>(a, p, mX, mY, st);
     default: return launch_split<TO, VEC, 1>(a, p, mX, mY, st);
   }
+}
+
+// Tokens up to which a pass over the weight beats the tensor cores' tiles: 4 of 4096 -> 4096 8.6 us against 8.3, of 768 -> 2304 3.6
+// against 4.5; 8 of 4096 -> 4096 14.2 against 8.4.  Channels per warp: 4096 -> 11008, two and four: 1 token 9.8 and 9.7 us, 2 tokens
+// 14.7 and 10.6, 4 tokens 21.2 and 14.7; 4096 -> 4096 5.7 and 6.5, 6.7 and 7.5, 9.5 and 9.9 (few warps).  One: 6.2, 8.7.
+constexpr int ROWS_MOST = 4, WIDE_ROWS = 8192;
+template <typename TO> cudaError_t launch_rows(const I8Args& a, const I8Params& p, cudaStream_t st) {
+  auto go = [&](auto kernel, int channels) {
+    return launch_overlapped(kernel, dim3((unsigned)((a.N + 8 * channels - 1) / (8 * channels))), dim3(256), 0, st, a.X, a.ldx, a.W, a.ldw, a.K, p);
+  };
+  if (a.M == 1) return go(gemm_i8_rows_kernel<TO, 1, 2>, 2);
+  if (a.N >= WIDE_ROWS) return a.M == 2 ? go(gemm_i8_rows_kernel<TO, 2, 4>, 4) : go(gemm_i8_rows_kernel<TO, 4, 4>, 4);
+  return a.M == 2 ? go(gemm_i8_rows_kernel<TO, 2, 2>, 2) : go(gemm_i8_rows_kernel<TO, 4, 2>, 2);
 }
 
 bool al16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -654,6 +736,7 @@ cudaError_t gemm_i8(const I8Args& a, int* status, cudaStream_t st) {
     if (a.dtype == DT_BF16) return launch_overlapped(gemm_i8_simt_kernel<bf16>, grid, dim3(256), 0, st, a.X, a.ldx, a.W, a.ldw, a.K, p);
     return launch_overlapped(gemm_i8_simt_kernel<float>, grid, dim3(256), 0, st, a.X, a.ldx, a.W, a.ldw, a.K, p);
   }
+  if (a.M <= ROWS_MOST) return a.dtype == DT_BF16 ? launch_rows<bf16>(a, p, st) : launch_rows<float>(a, p, st);
   if (a.dtype != DT_BF16) return launch_tc<float, false>(a, p, st);
   if (a.N % 8 == 0 && al16(a.Y) && al16(a.R)) return launch_tc<bf16, true>(a, p, st);
   return launch_tc<bf16, false>(a, p, st);
