@@ -74,25 +74,76 @@ template <typename TO> __device__ __forceinline__ void load_channel(const I8Para
   b = c < p.N && p.bias ? to_f<TO>(reinterpret_cast<const TO*>(p.bias)[c]) : 0.f;
 }
 
-// One 32-row x 32-column chunk of accumulators (acc: this thread's row, columns [n, n + 32)) to the output.  `stage`: 4 KB of this
-// warp.  Channel scales and biases arrive one per lane and go round through shared memory, which any N and type allow.
-// VEC: output (and residual) rows on 16-byte boundaries, bf16: staged like the bf16 layers' and stored by TMA.  Else each row of
-// the chunk leaves as one coalesced store of a warp.
-template <typename TO, bool VEC>
-__device__ __forceinline__ void i8_chunk(const I8Params& p, const uint32_t* acc, float sx, float sw_lane, float b_lane, int m_warp0, int n, int lane,
-                                         uint32_t stage, int& buf, const CUtensorMap* mapY) {
-  const uint32_t sbuf = VEC ? stage + (uint32_t)buf * 2048u : stage;
-  uint4 r[4];
-  if constexpr (VEC) {
-    if (p.R) {
-      const bf16* rrow = reinterpret_cast<const bf16*>(p.R) + (size_t)(m_warp0 + lane) * p.N + n;
+// The residual's part of a chunk, requested before the accumulators are awaited.  VEC: this thread's row, 16 bytes at a time; else
+// this thread's column.
+template <typename TO, bool VEC> struct Residual {
+  uint4 v[VEC ? 4 : 1];
+  TO s[VEC ? 1 : 32];
+  __device__ __forceinline__ void load(const I8Params& p, int m_warp0, int n, int lane) {
+    if (!p.R) return;
+    const TO* r = reinterpret_cast<const TO*>(p.R);
+    if constexpr (VEC) {
+      const bool in = m_warp0 + lane < p.M;
+      const uint4* row = reinterpret_cast<const uint4*>(r + (size_t)(m_warp0 + lane) * p.N + n);
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        r[j] = n + 8 * j < p.N && m_warp0 + lane < p.M ? __ldg(reinterpret_cast<const uint4*>(rrow + 8 * j)) : make_uint4(0u, 0u, 0u, 0u);
+      for (int j = 0; j < 4; ++j) v[j] = in && n + 8 * j < p.N ? __ldcs(row + j) : make_uint4(0u, 0u, 0u, 0u);
+    } else {
+      const TO* col = r + (size_t)m_warp0 * p.N + n + lane;
+#pragma unroll
+      for (int q = 0; q < 32; ++q) s[q] = n + lane < p.N && m_warp0 + q < p.M ? col[(size_t)q * p.N] : from_f<TO>(0.f);
     }
-    if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");     // the store that last read this buffer
+  }
+  // VEC: from a chunk that a copy has left in shared memory in the layout of stage_and_store
+  __device__ __forceinline__ void take(uint32_t rbuf, int lane) {
+    const uint32_t row = rbuf + (uint32_t)lane * 64u, sw = ((uint32_t)lane >> 1) & 3u;
+#pragma unroll
+    for (uint32_t j = 0; j < sizeof(v) / 16; ++j)
+      asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(v[j].x), "=r"(v[j].y), "=r"(v[j].z), "=r"(v[j].w) : "r"(row + ((j ^ sw) << 4)) : "memory");
+  }
+};
+
+// One 32-row x 32-column chunk of accumulators (acc: this thread's row, columns [n, n + 32)) to the output.  `stage`: 4 KB of this
+// warp.  Channel scales and biases arrive one per lane, requested a chunk ahead, and go round through shared memory (read from
+// global memory by every lane, where a chunk needs them, they made the epilogue the longer half of the kernel: 32768 x 1024 ->
+// 4096 128 us).  VEC: output and residual rows on 16-byte boundaries, bf16: staged like the bf16 layers' chunks and stored by TMA.
+template <typename TO>
+__device__ __forceinline__ void chunk_vec(const I8Params& p, const uint32_t* acc, float sx, float sw_lane, float b_lane, const Residual<TO, true>& res,
+                                          int m_warp0, int n, int lane, uint32_t stage, int& buf, const CUtensorMap* mapY) {
+  const uint32_t sbuf = stage + (uint32_t)buf * 2048u;
+  if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");       // the store that last read this buffer
+  __syncwarp();
+  sts1(sbuf + 4u * lane, sw_lane);
+  sts1(sbuf + 128u + 4u * lane, b_lane);
+  __syncwarp();
+  uint32_t packed[16];
+  const uint64_t sx2 = pack2(sx, sx);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float w[4], b[4];
+    lds4(w, sbuf + 16u * j);
+    lds4(b, sbuf + 128u + 16u * j);
+    const uint32_t rw[2] = {j & 1 ? res.v[j / 2].z : res.v[j / 2].x, j & 1 ? res.v[j / 2].w : res.v[j / 2].y};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const uint64_t a2 = pack2(__int2float_rn((int)acc[4 * j + 2 * i]), __int2float_rn((int)acc[4 * j + 2 * i + 1]));
+      uint64_t v = fma2(a2, mul2(sx2, pack2(w[2 * i], w[2 * i + 1])), pack2(b[2 * i], b[2 * i + 1]));
+      if (p.R) v = add2(v, bf16x2_to_f32x2(rw[i]));
+      float y0, y1;
+      unpack2(v, y0, y1);
+      const __nv_bfloat162 y2 = __floats2bfloat162_rn(y0, y1);
+      packed[2 * j + i] = *reinterpret_cast<const uint32_t*>(&y2);
+    }
   }
   __syncwarp();
+  stage_and_store(sbuf, mapY, packed, lane, n, m_warp0);         // clipped at row M and column N
+  buf ^= 1;
+}
+
+// Any N, alignment and type: channel scales and biases arrive one per lane and go round through shared memory, and each row of the
+// chunk leaves as one coalesced store of the warp.
+template <typename TO>
+__device__ __forceinline__ void chunk_any(const I8Params& p, const uint32_t* acc, float sx, float sw_lane, float b_lane, const Residual<TO, false>& res,
+                                          int m_warp0, int n, int lane, uint32_t sbuf) {
   sts1(sbuf + 4u * lane, sw_lane);
   sts1(sbuf + 128u + 4u * lane, b_lane);
   __syncwarp();
@@ -106,92 +157,59 @@ __device__ __forceinline__ void i8_chunk(const I8Params& p, const uint32_t* acc,
     for (int i = 0; i < 4; ++i) v[4 * j + i] = fmaf(__int2float_rn((int)acc[4 * j + i]), sx * w[i], b[i]);
   }
   __syncwarp();
-  if constexpr (VEC) {
-    if (p.R) {
+  // word (row, column) at column ^ row of its row: no two lanes of a store or a load share a bank
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const uint32_t w[4] = {r[j].x, r[j].y, r[j].z, r[j].w};
+  for (int i = 0; i < 32; ++i) sts1(sbuf + (uint32_t)lane * 128u + (uint32_t)((i ^ lane) << 2), v[i]);
+  __syncwarp();
+  if (n + lane < p.N) {
+    TO* y = reinterpret_cast<TO*>(p.Y) + (size_t)m_warp0 * p.N + n + lane;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { v[8 * j + 2 * i] += __uint_as_float(w[i] << 16); v[8 * j + 2 * i + 1] += __uint_as_float(w[i] & 0xffff0000u); }
-      }
+    for (int q = 0; q < 32; ++q) {
+      float t = lds1(sbuf + (uint32_t)q * 128u + (uint32_t)((lane ^ q) << 2));
+      if (p.R) t += to_f<TO>(res.s[q]);
+      if (m_warp0 + q < p.M) y[(size_t)q * p.N] = from_f<TO>(t);
     }
-    uint32_t packed[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      __nv_bfloat162 y2 = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      packed[i] = *reinterpret_cast<uint32_t*>(&y2);
-    }
-    stage_and_store(sbuf, mapY, packed, lane, n, m_warp0);       // clipped at row M and column N
-    buf ^= 1;
-  } else {
-    // word (row, column) at column ^ row of its row: no two lanes of a store or a load share a bank
-#pragma unroll
-    for (int i = 0; i < 32; ++i) sts1(sbuf + (uint32_t)lane * 128u + (uint32_t)((i ^ lane) << 2), v[i]);
-    __syncwarp();
-    const int rows = min(32, p.M - m_warp0);
-    TO* y = reinterpret_cast<TO*>(p.Y);
-    const TO* res = reinterpret_cast<const TO*>(p.R);
-    if (n + lane < p.N) {
-#pragma unroll 4
-      for (int q = 0; q < rows; ++q) {
-        const size_t at = (size_t)(m_warp0 + q) * p.N + n + lane;
-        float t = lds1(sbuf + (uint32_t)q * 128u + (uint32_t)((lane ^ q) << 2));
-        if (res) t += to_f<TO>(res[at]);
-        y[at] = from_f<TO>(t);
-      }
-    }
-    __syncwarp();
   }
-}
-
-// A warp's columns [c_begin, c_end) of the 32 rows from m_warp0 of a tile whose accumulator row is at t_row.
-template <typename TO, bool VEC>
-__device__ __forceinline__ void i8_tile(const I8Params& p, uint32_t t_row, float sx, int m_warp0, int n0, int c_begin, int c_end, int lane, uint32_t stage,
-                                        int& buf, const CUtensorMap* mapY, float sw, float b) {
-#pragma unroll 1
-  for (int c = c_begin; c < c_end; c += 32) {
-    const int n = n0 + c;
-    if (n >= p.N) break;
-    float sw_next = 0.f, b_next = 0.f;
-    if (c + 32 < c_end) load_channel<TO>(p, n + 32, lane, sw_next, b_next);
-    uint32_t acc[32];
-    tc_ld32(t_row + (uint32_t)c, reinterpret_cast<float*>(acc));
-    tc_wait_ld();
-    i8_chunk<TO, VEC>(p, acc, sx, sw, b, m_warp0, n, lane, stage, buf, mapY);
-    sw = sw_next; b = b_next;
-  }
+  __syncwarp();
 }
 
 // ------------------------------------------------------------------------------------------
 // CTA pairs
 // ------------------------------------------------------------------------------------------
-template <int BN_> struct PairCfg {
+// RES: a residual in VEC form.  Every epilogue warp has its 32 x 32 chunks brought into shared memory two ahead of their use: read row
+// by row from memory they took 191 us instead of (see below) at 32768 x 1024 -> 4096, where the product alone takes 111.
+template <int BN_, bool RES> struct PairCfg {
   static constexpr int BN = BN_;
   static constexpr int A_BYTES = TILE_BYTES;             // this CTA's 128 rows of x
   static constexpr int B_BYTES = (BN / 2) * KB;          // this CTA's half of the weight tile
   static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
-  static constexpr int STAGES = BN == 256 ? 6 : 8;
+  static constexpr int STAGES = (BN == 256 ? 6 : 8) - (RES ? BN == 256 ? 1 : 2 : 0);
+  static constexpr int R_BYTES = RES ? 8 * 2 * 2048 : 0;
   static constexpr int TMEM_COLS = 2 * BN;
-  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_STAGE_BYTES + 1024 + 256;
+  static constexpr int SMEM_BYTES = STAGES * STAGE_BYTES + EPI_STAGE_BYTES + R_BYTES + 1024 + 512;
+  static_assert(SMEM_BYTES <= 232448, "");
   static constexpr uint32_t IDESC = make_idesc_i8(2 * BM, BN);
 };
 
-template <typename TO, bool VEC, int BN>
+template <typename TO, bool VEC, bool RES, int BN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(NUM_THREADS, 1)
 gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_constant__ CUtensorMap mapW, const __grid_constant__ CUtensorMap mapY,
-                    I8Params p) {
-  using C = PairCfg<BN>;
+                    const __grid_constant__ CUtensorMap mapR, I8Params p) {
+  static_assert(VEC || !RES, "");
+  using C = PairCfg<BN, RES>;
   extern __shared__ uint8_t smem_raw[];
   const uint32_t raw = smem_u32(smem_raw);
   const uint32_t base = (raw + 1023u) & ~1023u;
   uint8_t* base_ptr = smem_raw + (base - raw);
   const uint32_t epi_base = base + C::STAGES * C::STAGE_BYTES;
-  const uint32_t bar_base = epi_base + EPI_STAGE_BYTES;
+  const uint32_t r_base = epi_base + EPI_STAGE_BYTES;
+  const uint32_t bar_base = r_base + C::R_BYTES;
   auto full_bar = [&](int s) { return bar_base + 8u * s; };                         // used in the leader
   auto empty_bar = [&](int s) { return bar_base + 8u * (C::STAGES + s); };          // one per CTA
   auto tfull_bar = [&](int a) { return bar_base + 8u * (2 * C::STAGES + a); };      // one per CTA
   auto tempty_bar = [&](int a) { return bar_base + 8u * (2 * C::STAGES + 2 + a); }; // used in the leader
-  uint8_t* tail = base_ptr + C::STAGES * C::STAGE_BYTES + EPI_STAGE_BYTES + 8 * (2 * C::STAGES + 4);
+  auto r_bar = [&](int w, int b) { return bar_base + 8u * (2 * C::STAGES + 4 + 2 * w + b); };     // RES: of epilogue warp w
+  uint8_t* tail = base_ptr + C::STAGES * C::STAGE_BYTES + EPI_STAGE_BYTES + C::R_BYTES + 8 * (2 * C::STAGES + 4 + 16);
   volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(tail);
   volatile int* abort_flag = reinterpret_cast<volatile int*>(tail + 8);
 
@@ -202,6 +220,7 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_const
   if (threadIdx.x == 0) {
     for (int s = 0; s < C::STAGES; ++s) { mbar_init(full_bar(s), 1); mbar_init(empty_bar(s), 1); }
     for (int a = 0; a < 2; ++a) { mbar_init(tfull_bar(a), 1); mbar_init(tempty_bar(a), 16); }
+    if (RES) for (int i = 0; i < 16; ++i) mbar_init(r_bar(i >> 1, i & 1), 1);
     *abort_flag = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -276,22 +295,89 @@ gemm_i8_pair_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_const
     const int q = warp & 3;
     const int half = (warp - 2) >> 2;
     const int c_begin = half * (BN / 2), c_end = c_begin + BN / 2;
+    const int ew = warp - 2;
     int as = 0; uint32_t aphase = 0;
-    const uint32_t stage = epi_base + (uint32_t)(warp - 2) * 4096u;
+    const uint32_t stage = epi_base + (uint32_t)ew * 4096u, rbuf = r_base + (uint32_t)ew * 4096u;
     int buf = 0;
     bool ok = true;
-    for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
+    auto rows_of = [&](int tile, int& n0) {
       int tm, tn; tile_coords(tile, p.tiles_m, p.tiles_n, tm, tn);
-      const int m_warp0 = tm * 2 * BM + (int)rank * BM + q * 32;
-      const int n0 = tn * BN;
+      n0 = tn * BN;
+      return tm * 2 * BM + (int)rank * BM + q * 32;
+    };
+    // RES: the chunks of this warp in the order of their use; `asked` counts those under way or done, `used` those done
+    int r_tile = pair, r_c = c_begin, asked = 0, used = 0;
+    auto ask = [&]() {
+      while (r_tile < num_tiles) {
+        int n0;
+        const int m = rows_of(r_tile, n0), n = n0 + r_c;
+        if (m >= p.M || n >= p.N) { r_tile += npairs; r_c = c_begin; continue; }      // what is left of this tile is outside
+        if (lane == 0) {
+          mbar_expect_tx(r_bar(ew, asked & 1), 2048);
+          tma_load_2d(rbuf + (uint32_t)(asked & 1) * 2048u, &mapR, r_bar(ew, asked & 1), n, m);
+        }
+        ++asked;
+        r_c += 32;
+        if (r_c >= c_end) { r_tile += npairs; r_c = c_begin; }
+        return;
+      }
+    };
+    if (RES) { ask(); ask(); }
+    for (int tile = pair; tile < num_tiles && ok; tile += npairs) {
+      int n0;
+      const int m_warp0 = rows_of(tile, n0);
       // in flight while the accumulator is awaited
       const float sx = m_warp0 + lane < p.M ? __ldg(p.sx + m_warp0 + lane) : 0.f;
-      float sw, b;
+      float sw = 0.f, b = 0.f;
       load_channel<TO>(p, n0 + c_begin, lane, sw, b);
       if (!mbar_wait(tfull_bar(as), aphase, abort_flag, p.status, 64)) { ok = false; break; }
       tc_fence_after();
       const uint32_t t_row = tmem_base + ((uint32_t)(q * 32) << 16) + (uint32_t)(as * BN);
-      if (m_warp0 < p.M) i8_tile<TO, VEC>(p, t_row, sx, m_warp0, n0, c_begin, c_end, lane, stage, buf, &mapY, sw, b);
+      if (m_warp0 < p.M) {
+        if constexpr (VEC) {
+          // accumulators one chunk ahead of their use
+          uint32_t acc[2][32];
+          tc_ld32(t_row + (uint32_t)c_begin, reinterpret_cast<float*>(acc[0]));
+#pragma unroll
+          for (int k = 0; k < BN / 64; ++k) {
+            const int c = c_begin + 32 * k, n = n0 + c;
+            if (n >= p.N || !ok) break;
+            tc_wait_ld();
+            float sw_next = 0.f, b_next = 0.f;
+            if (k + 1 < BN / 64) {
+              tc_ld32(t_row + (uint32_t)(c + 32), reinterpret_cast<float*>(acc[(k + 1) & 1]));
+              load_channel<TO>(p, n + 32, lane, sw_next, b_next);
+            }
+            Residual<TO, true> res;
+            if (RES) {
+              if (!mbar_wait(r_bar(ew, used & 1), (uint32_t)(used >> 1) & 1u, abort_flag, p.status, 65)) { ok = false; break; }
+              res.take(rbuf + (uint32_t)(used & 1) * 2048u, lane);
+              ++used;
+              asm volatile("fence.proxy.async.shared::cta;" ::: "memory");     // read before a copy writes the buffer again
+              __syncwarp();
+              ask();
+            }
+            chunk_vec<TO>(p, acc[k & 1], sx, sw, b, res, m_warp0, n, lane, stage, buf, &mapY);
+            sw = sw_next; b = b_next;
+          }
+          tc_wait_ld();                                // also where the last columns were past N
+        } else {
+#pragma unroll 1
+          for (int c = c_begin; c < c_end; c += 32) {
+            const int n = n0 + c;
+            if (n >= p.N) break;
+            Residual<TO, false> res;
+            res.load(p, m_warp0, n, lane);
+            float sw_next = 0.f, b_next = 0.f;
+            if (c + 32 < c_end) load_channel<TO>(p, n + 32, lane, sw_next, b_next);
+            uint32_t acc[32];
+            tc_ld32(t_row + (uint32_t)c, reinterpret_cast<float*>(acc));
+            tc_wait_ld();
+            chunk_any<TO>(p, acc, sx, sw, b, res, m_warp0, n, lane, stage);
+            sw = sw_next; b = b_next;
+          }
+        }
+      }
       tc_fence_before();
       __syncwarp();
       if (lane == 0) mbar_arrive_cluster(map_to_cta(tempty_bar(as), 0));   // 16 arrivals free the stage
@@ -419,9 +505,11 @@ gemm_i8_split_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_cons
   const bool live = warp >= 2 && m_warp0 < p.M && n < p.N;
   uint32_t acc[32];
   float sx = 0.f, sw = 0.f, b = 0.f;
+  Residual<TO, VEC> res;
   bool ok = false;
   if (warp >= 2) {
     if (live && owner == rank) {
+      res.load(p, m_warp0, n, lane);
       sx = m_warp0 + lane < p.M ? __ldg(p.sx + m_warp0 + lane) : 0.f;
       load_channel<TO>(p, n, lane, sw, b);
     }
@@ -459,9 +547,11 @@ gemm_i8_split_kernel(const __grid_constant__ CUtensorMap mapX, const __grid_cons
         }
       }
     }
-    int buf = 0;
     // the output staging takes the operand ring, which is idle: every product has completed
-    i8_chunk<TO, VEC>(p, acc, sx, sw, b, m_warp0, n, lane, base + (uint32_t)ew * 4096u, buf, &mapY);
+    const uint32_t stage = base + (uint32_t)ew * 4096u;
+    int buf = 0;
+    if constexpr (VEC) chunk_vec<TO>(p, acc, sx, sw, b, res, m_warp0, n, lane, stage, buf, &mapY);
+    else chunk_any<TO>(p, acc, sx, sw, b, res, m_warp0, n, lane, stage);
   }
   if (warp >= 2) epilogue_drain(lane);
 
@@ -600,6 +690,11 @@ bool map_codes(CUtensorMap* m, const void* ptr, int64_t rows, int64_t cols, int6
   return cached_map_2d_u8(m, ptr, rows, cols, ld, KB, box_rows, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B);
 }
 
+// output and residual: chunks of 32 x 32 in the epilogue's staging layout
+bool map_tile(CUtensorMap* m, const void* ptr, int64_t rows, int64_t cols, CUtensorMapL2promotion promo = CU_TENSOR_MAP_L2_PROMOTION_NONE) {
+  return cached_map_2d(m, ptr, rows, cols, cols, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B, promo);
+}
+
 template <typename K> int clusters_resident(K kernel, int size, int smem) {
   if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) return 0;
   cudaLaunchConfig_t cfg = {};
@@ -620,17 +715,24 @@ template <typename K> cudaError_t allow_smem(K kernel, PerDeviceOnce& once, int 
   return e;
 }
 
-template <typename TO, bool VEC, int BN> cudaError_t launch_pair(const I8Args& a, I8Params p, CUtensorMap mX, CUtensorMap mY, cudaStream_t st) {
-  using C = PairCfg<BN>;
+template <typename TO, bool VEC, bool RES, int BN> cudaError_t launch_pair_t(const I8Args& a, I8Params p, CUtensorMap mX, CUtensorMap mY, cudaStream_t st) {
+  using C = PairCfg<BN, RES>;
   static PerDeviceOnce once;
-  const cudaError_t e = allow_smem(gemm_i8_pair_kernel<TO, VEC, BN>, once, C::SMEM_BYTES);
+  const cudaError_t e = allow_smem(gemm_i8_pair_kernel<TO, VEC, RES, BN>, once, C::SMEM_BYTES);
   if (e != cudaSuccess) return e;
-  CUtensorMap mW;
+  CUtensorMap mW, mR = mY;
   if (!map_codes(&mW, a.W, a.N, a.K, a.ldw, BN / 2)) return cudaErrorInvalidValue;
+  // (a chunk's rows are 64 bytes: the next chunk's come into L2 with them)
+  if (RES && !map_tile(&mR, a.R, a.M, a.N, CU_TENSOR_MAP_L2_PROMOTION_L2_256B)) return cudaErrorInvalidValue;
   p.tiles_m = (a.M + 2 * BM - 1) / (2 * BM); p.tiles_n = (a.N + BN - 1) / BN;
   const int64_t tiles = (int64_t)p.tiles_m * p.tiles_n;
   const int most = g_pairs[current_device()], pairs = tiles < most ? (int)tiles : most;
-  return launch_overlapped(gemm_i8_pair_kernel<TO, VEC, BN>, dim3(2 * pairs), dim3(NUM_THREADS), C::SMEM_BYTES, st, mX, mW, mY, p);
+  return launch_overlapped(gemm_i8_pair_kernel<TO, VEC, RES, BN>, dim3(2 * pairs), dim3(NUM_THREADS), C::SMEM_BYTES, st, mX, mW, mY, mR, p);
+}
+template <typename TO, bool VEC, int BN> cudaError_t launch_pair(const I8Args& a, I8Params p, CUtensorMap mX, CUtensorMap mY, cudaStream_t st) {
+  if constexpr (VEC)
+    if (a.R) return launch_pair_t<TO, VEC, true, BN>(a, p, mX, mY, st);
+  return launch_pair_t<TO, VEC, false, BN>(a, p, mX, mY, st);
 }
 
 template <typename TO, bool VEC, int S> cudaError_t launch_split(const I8Args& a, I8Params p, CUtensorMap mX, CUtensorMap mY, cudaStream_t st) {
@@ -683,7 +785,7 @@ template <typename TO, bool VEC> cudaError_t launch_tc(const I8Args& a, I8Params
   p.x_rows = split && a.M < BM ? (a.M + 7) / 8 * 8 : BM;
   if (!map_codes(&mX, a.X, a.M, a.K, a.ldx, (uint32_t)p.x_rows)) return cudaErrorInvalidValue;
   mY = mX;
-  if (VEC && !cached_map_2d(&mY, a.Y, a.M, a.N, a.N, 32, 32, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE)) return cudaErrorInvalidValue;
+  if (VEC && !map_tile(&mY, a.Y, a.M, a.N)) return cudaErrorInvalidValue;
   switch (k) {
     case PICK_PAIR256: return launch_pair<TO, VEC, 256>(a, p, mX, mY, st);
     case PICK_PAIR128: return launch_pair<TO, VEC, 128>(a, p, mX, mY, st);
@@ -716,7 +818,7 @@ int gemm_i8_init() {
   const int dev = current_device(), sms = num_sms();
   if (dev < 0 || sms < 1) return -1;
   if (!g_once.needed(dev)) return 0;
-  const int pairs = clusters_resident(gemm_i8_pair_kernel<bf16, true, 256>, 2, PairCfg<256>::SMEM_BYTES);
+  const int pairs = clusters_resident(gemm_i8_pair_kernel<bf16, true, true, 256>, 2, PairCfg<256, true>::SMEM_BYTES);
   g_pairs[dev] = pairs < sms / 2 ? pairs : sms / 2;
   g_clusters[dev][0] = clusters_resident(gemm_i8_split_kernel<bf16, true, 2>, 2, SplitCfg<2>::SMEM_BYTES);
   g_clusters[dev][1] = clusters_resident(gemm_i8_split_kernel<bf16, true, 4>, 4, SplitCfg<4>::SMEM_BYTES);
