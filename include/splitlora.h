@@ -166,6 +166,16 @@ int splitlora_client_fwd(splitlora_ctx* ctx, const int32_t* tokens, void* act_ou
 int splitlora_server_step(splitlora_ctx* ctx, const void* act_in, const int32_t* labels,
                           void* act_grad_out, float* loss_out);
 
+/* A teacher for the server's loss: from the next server step on (the calls that contain one included) the loss of a position is
+ * that of splitlora_distill_loss with these weights and temperature instead of the plain cross-entropy, so that the server and, through
+ * dL/dS, the clients learn from a larger or unquantised model's outputs.  top_idx int32 and top_logits fp32, [K, b, T, k], DEVICE:
+ * the k largest logits of the teacher at each position (index outside [0, vocab): none there); read by every server step until
+ * replaced, so the caller may write the next round's values into the same buffers on the context's stream.  An ignored label
+ * leaves out its position for both terms.  Both pointers NULL: back to the cross-entropy.  1 <= k <= 256,
+ * 1e-3 <= temperature <= 1e3, finite weights. */
+int splitlora_set_teacher(splitlora_ctx* ctx, const int32_t* top_idx, const float* top_logits, int k, float temperature,
+                          float ce_weight, float kd_weight);
+
 /* Step a5, Eq. 6-7.  Back-propagates act_grad_in [K, b, T, d] through each client's blocks and
  * updates each client's adapters with lr_client.  Needs the saved state of the preceding
  * splitlora_client_fwd on this context, else SPLITLORA_ERR_STATE. */
@@ -270,6 +280,7 @@ int splitlora_launch_count(const splitlora_ctx* ctx, int64_t* launches);
 /* Per-kernel-class device time: when enabled, each launch is bracketed by CUDA events on the
  * context stream; splitlora_profile_report copies up to `cap` entries of {name, launches,
  * milliseconds} into HOST arrays and returns the number of classes in *n.
+ * The loss is "cross_entropy", or "distill_loss" where a teacher is set.
  * A norm and the rank-r projection behind it are "layernorm_fwd" and "lora_down_fwd", or, where one launch does both (few or
  * narrow rows), "layernorm_lora_down_fwd".
  * on: 0 off; 1 every launch class; 2 only the tensor-bound linear layers (classes "lora_linear_*",

@@ -37,7 +37,7 @@ EXPORTS = [
     "splitlora_library_status", "splitlora_set_client_cuts", "splitlora_lora_linear_bwd_parts",
     "splitlora_lora_linear_fwd_parts", "splitlora_quantize_rows", "splitlora_dequantize_rows",
     "splitlora_rmsnorm_quantize", "splitlora_rmsnorm_bwd_workspace_bytes", "splitlora_rmsnorm_bwd",
-    "splitlora_linear_i8", "splitlora_distill_loss",
+    "splitlora_linear_i8", "splitlora_distill_loss", "splitlora_set_teacher",
 ]
 
 
@@ -246,6 +246,22 @@ class SplitLoRA:
                                                   C.c_void_p(labels_host.data_ptr()), arr,
                                                   C.byref(loss) if want_loss else None))
         return loss.value if want_loss else None
+
+    def set_teacher(self, top_idx: Optional[torch.Tensor], top_logits: Optional[torch.Tensor] = None, temperature: float = 1.0,
+                    ce_weight: float = 0.5, kd_weight: float = 0.5):
+        """A teacher's top logits for the loss of the server step: top_idx int32 and top_logits fp32, [K, b, T, k] (None: back to
+        the cross-entropy); see splitlora_set_teacher.  The tensors are kept and read by every step until replaced."""
+        k = 0
+        if top_idx is not None:
+            c = self.cfg
+            k = int(top_idx.shape[-1])
+            shape = (c.n_clients, c.batch_per_client, c.seq, k)
+            for t, dt in ((top_idx, torch.int32), (top_logits, torch.float32)):
+                if t is None or t.dtype != dt or tuple(t.shape) != shape or t.device != self.workspace.device or not t.is_contiguous():
+                    raise SplitLoraError(ERR_ARG, f"set_teacher: contiguous int32 and float32 tensors {shape} on {self.workspace.device}")
+        self._check(self.lib.splitlora_set_teacher(self.ctx, _ptr(top_idx), _ptr(top_logits if top_idx is not None else None), k,
+                                                   C.c_float(temperature), C.c_float(ce_weight), C.c_float(kd_weight)))
+        self.teacher = (top_idx, top_logits) if top_idx is not None else None
 
     # ---- sharding hooks ----
     def set_loss_normalizer(self, n_valid_global: int):

@@ -119,6 +119,8 @@ struct splitlora_ctx {
   bool have_client_fwd = false;
   // sharding over devices: global loss normaliser (0: local count) and server update left to the caller
   int64_t loss_normalizer = 0;
+  // a teacher's top logits for the loss of the server step (top_idx null: plain cross-entropy)
+  struct { const int32_t* idx = nullptr; const float* logits = nullptr; int k = 0; float temperature = 1.f, ce = 1.f, kd = 0.f; } teacher;
   bool defer_server_update = false;
   std::vector<int> client_rank;             // per-client adapter rank (empty: every client has lora_r)
   int64_t round_index = 0, server_steps = 0, client_steps = 0;
@@ -1016,9 +1018,16 @@ int splitlora_server_step(splitlora_ctx* c, const void* act_in, const int32_t* l
   { GemmArgs a = base_args(c, c->xf, d, c->headw, d, c->logits, c->Vpad, M, c->Vpad, d);
     a.w_rows = c->V;
     CK(c, linear(c, "head_fwd", a)); }
-  { Scope s(c, "cross_entropy");
+  if (c->teacher.idx) {
+    Scope s(c, "distill_loss");
+    CK(c, distill(c->dt, c->logits, c->Vpad, labels, c->teacher.idx, c->teacher.logits, M, c->V, c->teacher.k, c->teacher.temperature,
+                  c->teacher.ce, c->teacher.kd, (int)c->loss_normalizer, c->logits, c->Vpad, c->row_loss, c->n_valid, c->loss_dev,
+                  c->status, c->st));
+  } else {
+    Scope s(c, "cross_entropy");
     CK(c, cross_entropy(c->dt, c->logits, c->Vpad, labels, M, c->V, c->row_loss, c->n_valid, c->loss_dev,
-                        (int)c->loss_normalizer, c->st)); }
+                        (int)c->loss_normalizer, c->st));
+  }
   // backward: head, final norm, blocks L-1 .. first
   { GemmArgs a = base_args(c, c->logits, c->Vpad, c->wteT, c->Vpad, c->g_a, d, M, d, c->Vpad);
     CK(c, linear(c, "head_bwd", a)); }
@@ -1191,6 +1200,23 @@ int splitlora_aggregate_broadcast(splitlora_ctx* c) {
 int splitlora_set_loss_normalizer(splitlora_ctx* c, int64_t n_valid_global) {
   if (!c || n_valid_global < 0 || n_valid_global > 2147483647LL) return SPLITLORA_ERR_ARG;
   c->loss_normalizer = n_valid_global;
+  return SPLITLORA_OK;
+}
+
+int splitlora_set_teacher(splitlora_ctx* c, const int32_t* top_idx, const float* top_logits, int k, float temperature, float ce_weight,
+                          float kd_weight) {
+  if (!c) return SPLITLORA_ERR_ARG;
+  if (!top_idx && !top_logits) {
+    c->teacher = {};
+    return SPLITLORA_OK;
+  }
+  if (!top_idx || !top_logits) return fail(c, SPLITLORA_ERR_ARG, "top_idx and top_logits go together");
+  if (k < 1 || k > DISTILL_MAX_K) return fail(c, SPLITLORA_ERR_ARG, "k must be in 1..256");
+  if (!(temperature >= 1e-3f && temperature <= 1e3f) || !std::isfinite(ce_weight) || !std::isfinite(kd_weight))
+    return fail(c, SPLITLORA_ERR_ARG, "temperature must be in [1e-3, 1e3] and the weights finite");
+  if (!aligned16(top_idx) || !aligned16(top_logits)) return fail(c, SPLITLORA_ERR_ALIGN, "teacher buffers not 16-byte aligned");
+  c->teacher.idx = top_idx; c->teacher.logits = top_logits; c->teacher.k = k;
+  c->teacher.temperature = temperature; c->teacher.ce = ce_weight; c->teacher.kd = kd_weight;
   return SPLITLORA_OK;
 }
 
