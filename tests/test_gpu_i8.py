@@ -23,7 +23,7 @@ def gen(seed):
 
 
 def randn(g, *shape, dtype=torch.float32):
-    return torch.randn(*shape, device="cuda", generator=g).to(dtype)
+    return torch.randn(*shape, device="cuda", generator=g, dtype=torch.float32).to(dtype)
 
 
 def offset(t, by):
@@ -77,7 +77,7 @@ def hard_rows(x):
                                  (9, 20000), (9, 65536), (9, 40001)])
 def test_quantize_rows(M, d, dtype):
     x = hard_rows(randn(gen(M + d), M, d)).to(dtype)
-    f = 0.5 + torch.rand(d, device="cuda", generator=gen(3))
+    f = 0.5 + torch.rand(d, device="cuda", generator=gen(3), dtype=torch.float32)
     for col in (None, f):
         codes, scales = B.quantize_rows(x, col_scale=col)
         v = x.float().cpu().numpy()
@@ -115,7 +115,7 @@ def test_quantize_rows_layouts(dtype):
 
 def norm_case(M, d, dtype, seed, residual):
     g = gen(seed)
-    x = hard_rows(randn(g, M, d) * (1 + 15 * (torch.rand(d, device="cuda", generator=g) < 0.02))).to(dtype)
+    x = hard_rows(randn(g, M, d) * (1 + 15 * (torch.rand(d, device="cuda", generator=g, dtype=torch.float32) < 0.02))).to(dtype)
     r = randn(g, M, d, dtype=dtype) if residual else None
     if residual and M > 3:
         r[1] = 0
@@ -284,10 +284,10 @@ def product64(x, sx, w, sw, bias, res):
 def run_product(M, K, N, dtype, sw=True, bias=True, res=True, padx=None, padw=None, extreme=False, off=0):
     g = gen(M + 3 * K + 7 * N)
     x, w = codes_case(M, K, M + K, padx, extreme), codes_case(N, K, N + K, padw, extreme)
-    sx = 0.01 + 0.02 * torch.rand(M, device="cuda", generator=g)
+    sx = 0.01 + 0.02 * torch.rand(M, device="cuda", generator=g, dtype=torch.float32)
     if M > 2:
         sx[M // 2] = 0
-    sw = 1e-3 * (0.5 + torch.rand(N, device="cuda", generator=g)) if sw else None
+    sw = 1e-3 * (0.5 + torch.rand(N, device="cuda", generator=g, dtype=torch.float32)) if sw else None
     b = randn(g, N, dtype=dtype) if bias else None
     r = randn(g, M, N, dtype=dtype) if res else None
     if off:
@@ -385,7 +385,7 @@ def distill64(z, idx, t, labels, T, wc, wk, n=0):
 def distill_case(M, V, k, dtype, seed, labels=True):
     g = gen(seed)
     z = (2.5 * randn(g, M, V)).to(dtype)
-    idx = torch.argsort(torch.rand(M, V, device="cuda", generator=g), dim=1)[:, :k].to(torch.int32).contiguous() if k <= V else \
+    idx = torch.argsort(torch.rand(M, V, device="cuda", generator=g, dtype=torch.float32), dim=1)[:, :k].to(torch.int32).contiguous() if k <= V else \
         torch.randint(0, V, (M, k), device="cuda", generator=g, dtype=torch.int32)
     t = (4 + 2 * randn(g, M, k)).contiguous()
     y = torch.randint(0, V, (M,), device="cuda", generator=g, dtype=torch.int32) if labels else None
@@ -600,8 +600,8 @@ def test_refusals_on_the_device():
               lambda: B.linear_i8(c, s, c, s, residual=x[:, :8].float()), lambda: B.rmsnorm_quantize(x, x[0, :8]), lambda: B.rmsnorm_quantize(x, x[0].float()),
               lambda: B.rmsnorm_bwd(x, x.float(), x[0]), lambda: B.distill_loss(x, c, x.float()),
               lambda: B.distill_loss(x, torch.zeros(8, 4, dtype=torch.int64, device="cuda"), x[:, :4].float()),
-              lambda: B.distill_loss(x, torch.zeros(8, 4, dtype=torch.int32, device="cuda"), torch.zeros(8, 4, device="cuda"), ce_weight=1.0),
-              lambda: B.distill_loss(x, torch.zeros(8, 4, dtype=torch.int32, device="cuda"), torch.zeros(8, 4, device="cuda"), temperature=0.0)):
+              lambda: B.distill_loss(x, torch.zeros(8, 4, dtype=torch.int32, device="cuda"), torch.zeros(8, 4, device="cuda", dtype=torch.float32), ce_weight=1.0),
+              lambda: B.distill_loss(x, torch.zeros(8, 4, dtype=torch.int32, device="cuda"), torch.zeros(8, 4, device="cuda", dtype=torch.float32), temperature=0.0)):
         with pytest.raises(B.SplitLoraError) as e:
             f()
         assert e.value.code == -1

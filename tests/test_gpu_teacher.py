@@ -144,7 +144,7 @@ def test_teacher_refusals():
     idx, t = (torch.from_numpy(a).cuda() for a in make_teacher(w, 8))
     for args, kw in (((idx.long(), t), {}), ((idx, t.half()), {}), ((idx, None), {}), ((idx[:, :, :-1], t), {}), ((idx.cpu(), t.cpu()), {}),
                      ((idx, t), {"temperature": 0.0}), ((idx, t), {"temperature": float("nan")}), ((idx, t), {"ce_weight": float("inf")}),
-                     ((torch.zeros(idx.shape[:-1] + (257,), dtype=torch.int32, device="cuda"), torch.zeros(idx.shape[:-1] + (257,), device="cuda")), {})):
+                     ((torch.zeros(idx.shape[:-1] + (257,), dtype=torch.int32, device="cuda"), torch.zeros(idx.shape[:-1] + (257,), dtype=torch.float32, device="cuda")), {})):
         with pytest.raises(B.SplitLoraError) as e:
             eng.set_teacher(*args, **kw)
         assert e.value.code == -1

@@ -103,7 +103,7 @@ def test_distill_refuses(bad, code):
 def test_binding_refuses_tensors_off_the_device():
     import torch
     if torch.cuda.is_available():
-        x = torch.zeros(4, 64)                     # on the host
+        x = torch.zeros(4, 64, dtype=torch.float32)                     # on the host
         for f in (lambda: B.quantize_rows(x), lambda: B.rmsnorm_quantize(x, x[0]), lambda: B.rmsnorm_bwd(x, x, x[0])):
             with pytest.raises(B.SplitLoraError) as e:
                 f()
@@ -111,4 +111,4 @@ def test_binding_refuses_tensors_off_the_device():
     with pytest.raises(B.SplitLoraError):
         B.quantize_rows(torch.zeros(4, 64, dtype=torch.float64))
     with pytest.raises(B.SplitLoraError):
-        B.quantize_rows(torch.zeros(64))
+        B.quantize_rows(torch.zeros(64, dtype=torch.float32))
