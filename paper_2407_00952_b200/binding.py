@@ -550,22 +550,44 @@ def _matrix(what: str, x: torch.Tensor):
 
 def empty_codes(M: int, d: int) -> torch.Tensor:
     """int8 [M, d] whose rows start on 16-byte boundaries (what lets linear_i8 run on the tensor cores)."""
-    ld = (d + 15) // 16 * 16
-    t = torch.empty(M, ld, dtype=_I8, device="cuda")       # (dimensions one by one: 0.7 us less than as a tuple)
-    return t if ld == d else t[:, :d]
+    if d % 16 == 0:
+        return torch.empty(M, d, dtype=_I8, device="cuda")       # (dimensions one by one: 0.7 us less than as a tuple)
+    return torch.empty_strided((M, d), ((d + 15) // 16 * 16, 1), dtype=_I8, device="cuda")
+
+
+# Buffers that a call makes itself are not checked again.
+def _codes_out(codes: Optional[torch.Tensor], M: int, d: int, dev: int):
+    """(codes, address, distance of rows): the caller's buffer, or a new one."""
+    if codes is None:
+        codes = empty_codes(M, d)
+        return codes, codes.data_ptr(), (d + 15) // 16 * 16
+    p, ld = _codes_in("codes", codes, M, d, dev)
+    return codes, p, ld
+
+
+def _scales_out(scales: Optional[torch.Tensor], M: int, dev: int):
+    if scales is None:
+        scales = torch.empty(M, dtype=_F32, device=dev)
+        return scales, scales.data_ptr()
+    return scales, _in("scales", scales, _F32, (M,), dev)
+
+
+def _like_out(what: str, t: Optional[torch.Tensor], x: torch.Tensor, shape, dev: int):
+    if t is None:
+        t = torch.empty_like(x)
+        return t, t.data_ptr()
+    return t, _in(what, t, x.dtype, shape, dev)
 
 
 def quantize_rows(x: torch.Tensor, col_scale: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
                   scales: Optional[torch.Tensor] = None):
     """x [M, d] -> (codes int8 [M, d], scales fp32 [M]); col_scale fp32 [d] multiplies x first (splitlora_quantize_rows)."""
     dt, M, d, dev = _matrix("x", x)
-    if codes is None:
-        codes = empty_codes(M, d)
-    if scales is None:
-        scales = torch.empty(M, dtype=_F32, device=dev)
-    cp, ld = _codes_in("codes", codes, M, d, dev)
-    rc = load().splitlora_quantize_rows(dt, _in("x", x, x.dtype, (M, d), dev), _in("col_scale", col_scale, _F32, (d,), dev), M, d, cp, ld,
-                                        _in("scales", scales, _F32, (M,), dev), _raw_stream(dev))
+    xp = _in("x", x, x.dtype, (M, d), dev)
+    fp = 0 if col_scale is None else _in("col_scale", col_scale, _F32, (d,), dev)
+    codes, cp, ld = _codes_out(codes, M, d, dev)
+    scales, sp = _scales_out(scales, M, dev)
+    rc = load().splitlora_quantize_rows(dt, xp, fp, M, d, cp, ld, sp, _raw_stream(dev))
     if rc:
         _rc(rc, "quantize_rows")
     return codes, scales
@@ -592,19 +614,18 @@ def rmsnorm_quantize(x: torch.Tensor, g: torch.Tensor, residual: Optional[torch.
     """RMSNorm of x + residual as int8 codes (splitlora_rmsnorm_quantize): (codes, scales, h, y).  h is the sum (None without a
     residual, unless a buffer is passed), y the normalised row in x's dtype (None unless want_y or a buffer is passed)."""
     dt, M, d, dev = _matrix("x", x)
-    t = x.dtype
-    if codes is None:
-        codes = empty_codes(M, d)
-    if scales is None:
-        scales = torch.empty(M, dtype=_F32, device=dev)
-    if h is None and residual is not None:
-        h = torch.empty_like(x)
-    if y is None and want_y:
-        y = torch.empty_like(x)
-    cp, ld = _codes_in("codes", codes, M, d, dev)
-    rc = load().splitlora_rmsnorm_quantize(
-        dt, _in("x", x, t, (M, d), dev), _in("residual", residual, t, (M, d), dev), _in("g", g, t, (d,), dev), eps, M, d,
-        _in("h", h, t, (M, d), dev), _in("y", y, t, (M, d), dev), cp, ld, _in("scales", scales, _F32, (M,), dev), _raw_stream(dev))
+    t, shape = x.dtype, (M, d)
+    xp, gp = _in("x", x, t, shape, dev), _in("g", g, t, (d,), dev)
+    rp = hp = yp = 0
+    if residual is not None:
+        rp = _in("residual", residual, t, shape, dev)
+    codes, cp, ld = _codes_out(codes, M, d, dev)
+    scales, sp = _scales_out(scales, M, dev)
+    if h is not None or residual is not None:
+        h, hp = _like_out("h", h, x, shape, dev)
+    if y is not None or want_y:
+        y, yp = _like_out("y", y, x, shape, dev)
+    rc = load().splitlora_rmsnorm_quantize(dt, xp, rp, gp, eps, M, d, hp, yp, cp, ld, sp, _raw_stream(dev))
     if rc:
         _rc(rc, "rmsnorm_quantize")
     return codes, scales, h, y
@@ -615,9 +636,10 @@ def rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, g: torch.Tensor, resid: Optio
     """Gradient of rmsnorm_quantize with respect to x (= residual) and, where want_dg, to g in fp32: (dx, dg or None)
     (splitlora_rmsnorm_bwd); resid: the gradient that reaches h by itself."""
     dt, M, d, dev = _matrix("h", h)
-    t = h.dtype
-    if dx is None:
-        dx = torch.empty_like(h)
+    t, shape = h.dtype, (M, d)
+    yp, hp, gp = _in("dy", dy, t, shape, dev), _in("h", h, t, shape, dev), _in("g", g, t, (d,), dev)
+    rp = 0 if resid is None else _in("resid", resid, t, shape, dev)
+    dx, xp = _like_out("dx", dx, h, shape, dev)
     dg, dgp, wsp, ws_bytes = None, 0, 0, 0
     if want_dg:
         dg = torch.empty(d, dtype=_F32, device=dev)
@@ -628,9 +650,7 @@ def rmsnorm_bwd(dy: torch.Tensor, h: torch.Tensor, g: torch.Tensor, resid: Optio
             workspace = torch.empty(n.value, dtype=torch.uint8, device=dev)
         wsp = _in("workspace", workspace, workspace.dtype, workspace.shape, dev)
         ws_bytes = workspace.numel() * workspace.element_size()
-    rc = load().splitlora_rmsnorm_bwd(
-        dt, _in("dy", dy, t, (M, d), dev), _in("h", h, t, (M, d), dev), _in("g", g, t, (d,), dev), _in("resid", resid, t, (M, d), dev), eps, M, d,
-        _in("dx", dx, t, (M, d), dev), dgp, wsp, ws_bytes, _raw_stream(dev))
+    rc = load().splitlora_rmsnorm_bwd(dt, yp, hp, gp, rp, eps, M, d, xp, dgp, wsp, ws_bytes, _raw_stream(dev))
     if rc:
         _rc(rc, "rmsnorm_bwd")
     return dx, dg
@@ -646,14 +666,21 @@ def linear_i8(x: torch.Tensor, x_scales: torch.Tensor, W: torch.Tensor, w_scales
     M, K = x.shape
     N = W.shape[0]
     if y is None:
-        y = torch.empty(M, N, dtype=dtype, device="cuda")
-    dt, _, _, dev = _matrix("y", y)
-    t = y.dtype
+        dt, dev = _DTYPE_ID.get(dtype), torch.cuda.current_device()
+        if dt is None:
+            raise SplitLoraError(ERR_ARG, f"linear_i8: output of type {dtype}")
+        t, y = dtype, torch.empty(M, N, dtype=dtype, device=dev)
+        yp = y.data_ptr()
+    else:
+        dt, _, _, dev = _matrix("y", y)
+        t = y.dtype
+        yp = _in("y", y, t, (M, N), dev)
     xp, ldx = _codes_in("x", x, M, K, dev)
     wp, ldw = _codes_in("W", W, N, K, dev)
     rc = load().splitlora_linear_i8(
-        dt, xp, ldx, _in("x_scales", x_scales, _F32, (M,), dev), wp, ldw, _in("w_scales", w_scales, _F32, (N,), dev), _in("bias", bias, t, (N,), dev),
-        _in("residual", residual, t, (M, N), dev), M, K, N, _in("y", y, t, (M, N), dev), _raw_stream(dev))
+        dt, xp, ldx, _in("x_scales", x_scales, _F32, (M,), dev), wp, ldw, 0 if w_scales is None else _in("w_scales", w_scales, _F32, (N,), dev),
+        0 if bias is None else _in("bias", bias, t, (N,), dev), 0 if residual is None else _in("residual", residual, t, (M, N), dev), M, K, N, yp,
+        _raw_stream(dev))
     if rc:
         _rc(rc, "linear_i8")
     return y
@@ -670,14 +697,14 @@ def distill_loss(logits: torch.Tensor, top_idx: torch.Tensor, top_logits: torch.
         raise SplitLoraError(ERR_ARG, "top_idx is a matrix [M, k]")
     k = top_idx.shape[1]
     t = logits.dtype
-    if dlogits is None:
-        dlogits = torch.empty_like(logits)
+    zp = _in("logits", logits, t, (M, ld), dev)
+    dlogits, dp = _like_out("dlogits", dlogits, logits, (M, ld), dev)
     out = torch.empty(M + 2, dtype=_F32, device=dev)       # row losses, loss, count
     p = out.data_ptr()
     rc = load().splitlora_distill_loss(
-        dt, _in("logits", logits, t, (M, ld), dev), ld, _in("labels", labels, _I32, (M,), dev), _in("top_idx", top_idx, _I32, (M, k), dev),
+        dt, zp, ld, 0 if labels is None else _in("labels", labels, _I32, (M,), dev), _in("top_idx", top_idx, _I32, (M, k), dev),
         _in("top_logits", top_logits, _F32, (M, k), dev), M, ld if vocab is None else int(vocab), k, temperature, ce_weight, kd_weight, normalizer,
-        _in("dlogits", dlogits, t, (M, ld), dev), ld, p, p + 4 * M, p + 4 * M + 4, _raw_stream(dev))
+        dp, ld, p, p + 4 * M, p + 4 * M + 4, _raw_stream(dev))
     if rc:
         _rc(rc, "distill_loss")
     return out[M], out[:M], dlogits
