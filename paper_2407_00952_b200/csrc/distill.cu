@@ -236,12 +236,18 @@ distill_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p
 // Persistent blocks walk the rows.  One thread copies the next rows into a ring of one or two buffers with bulk copies; a row's
 // logits are read from there twice (maximum, exponentials), the exponentials of a temperature stay in registers until the
 // row's sums are known, and the gradient leaves from there: a logit costs HBM one read and one write, and one exponential where
-// one temperature is enough or the two are 1 and 2 (then e^z = (e^(z/2))^2).  What bounds the streaming kernel above is the
+// one temperature is enough or the two are 1 and 2, 3 or 4 (then e^z = (e^(z/2))^2 and so on).  What bounds the streaming kernel above is the
 // exponential unit and instruction issue (4 exponentials per logit) as much as traffic.
 // Rows may start anywhere (a vocabulary of 50257 entries in contiguous rows): a row is held as the 16-byte vectors that cover it, its
 // first and last vector patched by the threads that own them; the copies take whole vectors inside the buffer and plain
 // loads the ragged ends of the first and last row.
-enum { EXP_HALF = 2 };   // temperatures 1 and 2
+// Modes from 2 on: temperatures 1 and `mode` (2, 3 or 4): e^z is that power of e^(z / mode).
+enum { EXP_POWERS = 2, EXP_MOST = 4 };
+template <int MODE> __device__ __forceinline__ float power(float x) { return MODE == 2 ? x * x : MODE == 3 ? x * x * x : (x * x) * (x * x); }
+template <int MODE> __device__ __forceinline__ uint64_t power2(uint64_t x) {
+  const uint64_t s = tc::mul2(x, x);
+  return MODE == 2 ? s : MODE == 3 ? tc::mul2(s, x) : tc::mul2(s, s);
+}
 
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
   asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
@@ -273,9 +279,13 @@ template <typename T, int THREADS, int MINB, int MODE>
 __global__ void __launch_bounds__(THREADS, MINB)
 distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p, int M, int nbuf, int buf_bytes, int* status) {
   constexpr int W = Vec16<T>::N, NW = THREADS / 32, ISSUER = THREADS - 32;
-  extern __shared__ __align__(128) uint8_t smem[];       // nbuf rows
-  __shared__ __align__(16) int sh_idx[SLOTS][DISTILL_MAX_K];
-  __shared__ float sh_q[SLOTS][DISTILL_MAX_K], sh_z[2][DISTILL_MAX_K];
+  constexpr int UNROLL = THREADS > 128 ? 4 : 2;          // many blocks in different places of their rows: the code has to stay cached
+  extern __shared__ __align__(128) uint8_t smem[];       // nbuf rows, then the tables of the teacher's entries
+  const int k4 = (p.k + 3) / 4 * 4;
+  int* tables = reinterpret_cast<int*>(smem + (size_t)nbuf * buf_bytes);
+  auto sh_idx = [&](int slot) { return tables + slot * k4; };
+  auto sh_q = [&](int slot) { return reinterpret_cast<float*>(tables + (SLOTS + slot) * k4); };
+  auto sh_z = [&](int par) { return reinterpret_cast<float*>(tables + (2 * SLOTS + par) * k4); };
   __shared__ float sh_m[2][NW], sh_sT[2][NW], sh_s1[2][NW];
   __shared__ T sh_edge[2][2][W];                         // logits of the row's ragged first and last vector
   __shared__ float sh_zy[2], sh_f1[2], sh_fT[2], sh_base[2], sh_fq[2];
@@ -323,8 +333,8 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
   // warp 1: a row's teacher entries into the tables; lane j % 32 copies entry j and is the one that reads it
   auto fetch_teacher = [&](int row, int slot) {
     for (int j = lane; j < k; j += 32) {
-      cp_async4(tc::smem_u32(&sh_idx[slot][j]), p.idx + (int64_t)row * k + j);
-      cp_async4(tc::smem_u32(&sh_q[slot][j]), p.t + (int64_t)row * k + j);
+      cp_async4(tc::smem_u32(&sh_idx(slot)[j]), p.idx + (int64_t)row * k + j);
+      cp_async4(tc::smem_u32(&sh_q(slot)[j]), p.t + (int64_t)row * k + j);
     }
   };
   // warp 1: t -> q = softmax(t / T) over the row's entries, absent ones as index -1
@@ -332,20 +342,20 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
     asm volatile("cp.async.wait_all;" ::: "memory");
     float tmax = -INFINITY, tsum = 0.f;
     for (int j = lane; j < k; j += 32) {
-      const int v = sh_idx[slot][j];
+      const int v = sh_idx(slot)[j];
       const bool ok = v >= 0 && v < V;
-      const float t = ok ? sh_q[slot][j] : -INFINITY;
-      if (!ok) { sh_idx[slot][j] = -1; sh_q[slot][j] = t; }
+      const float t = ok ? sh_q(slot)[j] : -INFINITY;
+      if (!ok) { sh_idx(slot)[j] = -1; sh_q(slot)[j] = t; }
       tmax = t != t || tmax != tmax ? __uint_as_float(0x7fffffffu) : fmaxf(tmax, t);
     }
-    for (int j = k + lane; j < (k + 3) / 4 * 4; j += 32) sh_idx[slot][j] = -1;
+    for (int j = k + lane; j < k4; j += 32) sh_idx(slot)[j] = -1;
     const bool nan = __any_sync(0xffffffffu, tmax != tmax);
     tmax = warp_max_redux(nan ? 0.f : tmax);
     if (nan) tmax = __uint_as_float(0x7fffffffu);
     const bool teach = tmax != -INFINITY && p.wk != 0.f;     // else the teacher says nothing about this row
-    for (int j = lane; j < k; j += 32) tsum += teach ? expf((sh_q[slot][j] - tmax) * p.inv_t) : 0.f;
+    for (int j = lane; j < k; j += 32) tsum += teach ? expf((sh_q(slot)[j] - tmax) * p.inv_t) : 0.f;
     tsum = warp_sum(tsum);
-    for (int j = lane; j < k; j += 32) sh_q[slot][j] = teach ? expf((sh_q[slot][j] - tmax) * p.inv_t) / tsum : 0.f;
+    for (int j = lane; j < k; j += 32) sh_q(slot)[j] = teach ? expf((sh_q(slot)[j] - tmax) * p.inv_t) / tsum : 0.f;
     if (lane == 0) { sh_teach[slot] = teach; sh_tmax[slot] = tmax; sh_lts[slot] = logf(tsum); }
   };
   // from warp 2 on: the entries of a row that carry a target; the first entry of an index writes for all of them
@@ -353,20 +363,20 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
     const float f1 = sh_f1[par], fT = sh_fT[par], base = sh_base[par];
     T* out = grad + row * p.ldo;
     for (int j = tid - 64; j <= k; j += THREADS - 64) {
-      const int v = j < k ? sh_idx[slot][j] : p.labels ? y : -1;       // entry k: the label
+      const int v = j < k ? sh_idx(slot)[j] : p.labels ? y : -1;       // entry k: the label
       if (v < 0) continue;
       bool first = true;
       float q = 0.f;
       for (int i = 0; i < k; i += 4) {
-        const int4 w = *reinterpret_cast<const int4*>(&sh_idx[slot][i]);
-        if (w.x == v) { if (i < j) first = false; q += sh_q[slot][i]; }
-        if (w.y == v) { if (i + 1 < j) first = false; q += sh_q[slot][i + 1]; }
-        if (w.z == v) { if (i + 2 < j) first = false; q += sh_q[slot][i + 2]; }
-        if (w.w == v) { if (i + 3 < j) first = false; q += sh_q[slot][i + 3]; }
+        const int4 w = *reinterpret_cast<const int4*>(&sh_idx(slot)[i]);
+        if (w.x == v) { if (i < j) first = false; q += sh_q(slot)[i]; }
+        if (w.y == v) { if (i + 1 < j) first = false; q += sh_q(slot)[i + 1]; }
+        if (w.z == v) { if (i + 2 < j) first = false; q += sh_q(slot)[i + 2]; }
+        if (w.w == v) { if (i + 3 < j) first = false; q += sh_q(slot)[i + 3]; }
       }
       if (!first) continue;
-      const float z = (j < k ? sh_z[par][j] : sh_zy[par]) - base, x = ex2(z * p.cT);
-      float r = MODE == EXP_ONE ? f1 * x : MODE == EXP_HALF ? x * fmaf(x, f1, fT) : fmaf(f1, ex2(z * p.c1), fT * x);
+      const float z = (j < k ? sh_z(par)[j] : sh_zy[par]) - base, x = ex2(z * p.cT);
+      float r = MODE == EXP_ONE ? f1 * x : fmaf(f1, MODE == EXP_TWO ? ex2(z * p.c1) : power<MODE>(x), fT * x);
       r -= sh_fq[par] * q;
       if (p.labels && v == y) r -= p.wc * inv_n;
       out[v] = from_f<T>(r);
@@ -442,7 +452,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
       float m = -INFINITY;
       if constexpr (W == 8) {
         __nv_bfloat162 m2 = __floats2bfloat162_rn(-INFINITY, -INFINITY);
-#pragma unroll 4
+#pragma unroll UNROLL
         for (int v = tid; v < nvec; v += THREADS) {
           Vec16<T> r; r.load(zs + (size_t)v * W);
           const __nv_bfloat162* h2 = reinterpret_cast<const __nv_bfloat162*>(&r.raw);
@@ -450,7 +460,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
         }
         m = fmaxf(__low2float(m2), __high2float(m2));
       } else {
-#pragma unroll 4
+#pragma unroll UNROLL
         for (int v = tid; v < nvec; v += THREADS) {
           Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
@@ -461,7 +471,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
       uint64_t sT2 = 0ull, s12 = 0ull;
       {
         const uint64_t neg2 = tc::pack2(-mine, -mine);
-#pragma unroll 4
+#pragma unroll UNROLL
         for (int v = tid; v < nvec; v += THREADS) {
           Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
@@ -469,7 +479,8 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
             const uint64_t dd = tc::add2(pair_of(r, i), neg2);       // z - maximum
             const uint64_t e = exp_pair(tc::mul2(dd, cT2));
             sT2 = tc::add2(sT2, e);
-            if constexpr (MODE == EXP_HALF) s12 = tc::fma2(e, e, s12);
+            if constexpr (MODE == 2) s12 = tc::fma2(e, e, s12);
+            if constexpr (MODE > 2) s12 = tc::add2(s12, power2<MODE>(e));
             if constexpr (MODE == EXP_TWO) s12 = tc::add2(s12, exp_pair(tc::mul2(dd, c12)));
           }
         }
@@ -486,7 +497,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
       {
         const float f = factor(m, wbase, p.cT);
         sT = warp_sum(sT * f);
-        if constexpr (MODE == EXP_HALF) s1 = warp_sum(s1 * (f * f));
+        if constexpr (MODE >= EXP_POWERS) s1 = warp_sum(s1 * power<MODE>(f));
         if constexpr (MODE == EXP_TWO) s1 = warp_sum(s1 * factor(m, wbase, p.c1));
       }
       if (lane == 0) {
@@ -504,7 +515,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
         base = m == -INFINITY ? 0.f : m;
         const float f = factor(rm, base, p.cT);
         sT *= f;
-        if constexpr (MODE == EXP_HALF) s1 *= f * f;
+        if constexpr (MODE >= EXP_POWERS) s1 *= power<MODE>(f);
         if constexpr (MODE == EXP_TWO) s1 *= factor(rm, base, p.c1);
 #pragma unroll
         for (int o = NW / 2; o > 0; o >>= 1) {
@@ -519,9 +530,9 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
         const float log_sT = logf(sT), tmax = sh_tmax[slot], lts = sh_lts[slot], *t = p.t + (int64_t)row * k;
         float kl = 0.f;
         for (int j = lane; j < k; j += 32) {
-          const int v = sh_idx[slot][j];
-          const float q = sh_q[slot][j], z = v >= 0 ? to_f<T>(zs[s + v]) : 0.f;
-          sh_z[par][j] = z;
+          const int v = sh_idx(slot)[j];
+          const float q = sh_q(slot)[j], z = v >= 0 ? to_f<T>(zs[s + v]) : 0.f;
+          sh_z(par)[j] = z;
           // T times the divergence: (z - base) / T could overflow
           if (q != 0.f) kl += q * fmaf(p.temp, ((t[j] - tmax) * p.inv_t - lts) + log_sT, base - z);
         }
@@ -538,7 +549,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
           const int which = lane / W, i = lane % W, q = (which ? last * W : 0) + i;
           if ((which ? ragged_last : ragged_first && !(last == 0 && ragged_last)) && q >= s && q < end) {
             const float z = to_f<T>(sh_edge[par][which][i]) - base, x = ex2(z * p.cT);
-            out[q] = from_f<T>(MODE == EXP_ONE ? f1 * x : MODE == EXP_HALF ? x * fmaf(x, f1, fT) : fmaf(f1, ex2(z * p.c1), fT * x));
+            out[q] = from_f<T>(MODE == EXP_ONE ? f1 * x : fmaf(f1, MODE == EXP_TWO ? ex2(z * p.c1) : power<MODE>(x), fT * x));
           }
         }
         __syncwarp();
@@ -550,7 +561,7 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
       // ---- gradient
       const uint64_t f12 = tc::pack2(f1, f1), fT2 = tc::pack2(fT, fT), neg2 = tc::pack2(-base, -base);
       const int v_to = ragged_last ? last : nvec;
-#pragma unroll 4
+#pragma unroll UNROLL
       for (int v = tid == 0 && ragged_first ? THREADS : tid; v < v_to; v += THREADS) {
         Vec16<T> r, o;
         r.load(zs + (size_t)v * W);
@@ -560,7 +571,8 @@ distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillA
           const uint64_t e = exp_pair(tc::mul2(dd, cT2));
           uint64_t w;
           if constexpr (MODE == EXP_ONE) w = tc::mul2(e, f12);
-          if constexpr (MODE == EXP_HALF) w = tc::mul2(e, tc::fma2(e, f12, fT2));
+          if constexpr (MODE == 2) w = tc::mul2(e, tc::fma2(e, f12, fT2));
+          if constexpr (MODE > 2) w = tc::fma2(power2<MODE>(e), f12, tc::mul2(e, fT2));
           if constexpr (MODE == EXP_TWO) w = tc::fma2(e, fT2, tc::mul2(f12, exp_pair(tc::mul2(dd, c12))));
           float a, c;
           tc::unpack2(w, a, c);
@@ -620,10 +632,11 @@ namespace {
 
 // Rows up to this many labels are counted by every block of the ring kernel instead of a launch in front of it.
 constexpr int COUNT_HERE = 4096;
-constexpr int RING_TABLES = 12800, RING_BYTES = 232448 - 1024 - RING_TABLES;     // static tables; dynamic shared memory of all blocks of an SM
+// Static shared memory of a block with what the system keeps per block, dynamic shared memory of a block, all of an SM's.
+constexpr int RING_STATIC = 4096, RING_BYTES = 232448 - 3072, SM_BYTES = 233472;
 
 template <typename T, int THREADS, int MINB, int MODE>
-cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, int buf, int nbuf, int fit, int* status, cudaStream_t st) {
+cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, int buf, int nbuf, int tables, int fit, int* status, cudaStream_t st) {
   const auto kernel = distill_ring_kernel<T, THREADS, MINB, MODE>;
   static PerDeviceOnce once;
   const int dev = current_device();
@@ -633,20 +646,24 @@ cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, i
     once.done(dev);
   }
   const int64_t most = (int64_t)num_sms() * (fit < MINB ? fit : MINB);
-  return launch_overlapped(kernel, dim3((unsigned)(M < most ? M : most)), dim3(THREADS), (size_t)nbuf * buf, st, logits, grad, p, M, nbuf, buf, status);
+  return launch_overlapped(kernel, dim3((unsigned)(M < most ? M : most)), dim3(THREADS), (size_t)nbuf * buf + tables, st, logits, grad, p, M, nbuf, buf, status);
 }
+
+int ring_buffer(int V, size_t es) { return (int)(((size_t)V * es + 15) / 16 * 16 + 16); }         // a row at any alignment
+int ring_tables(int k) { return (2 * SLOTS + 2) * ((k + 3) / 4 * 4) * 4; }
+bool ring_supported(int V, int k, size_t es) { return (int64_t)V * (int64_t)es + 32 + ring_tables(k) <= RING_BYTES; }
 
 // As many rows per SM as shared memory holds, up to eight; two buffers per row where eight rows have room for them.
 template <typename T, int MODE>
 cudaError_t ring(const T* logits, T* grad, const DistillArgs& p, int M, int* status, cudaStream_t st) {
-  const int buf = (int)(((size_t)p.V * sizeof(T) + 15) / 16 * 16 + 16);
-  const int one = (RING_BYTES + RING_TABLES) / (buf + RING_TABLES), two = (RING_BYTES + RING_TABLES) / (2 * buf + RING_TABLES);
-  if (two >= 8) return launch_ring<T, 128, 8, MODE>(logits, grad, p, M, buf, 2, two, status, st);
-  if (one >= 6) return launch_ring<T, 128, 8, MODE>(logits, grad, p, M, buf, 1, one, status, st);
-  if (one >= 4) return launch_ring<T, 128, 5, MODE>(logits, grad, p, M, buf, 1, one, status, st);
-  if (one == 3) return launch_ring<T, 256, 3, MODE>(logits, grad, p, M, buf, 1, one, status, st);
-  if (one == 2) return launch_ring<T, 256, 2, MODE>(logits, grad, p, M, buf, 1, one, status, st);
-  return launch_ring<T, 512, 1, MODE>(logits, grad, p, M, buf, 1, one, status, st);
+  const int buf = ring_buffer(p.V, sizeof(T)), tables = ring_tables(p.k);
+  const int one = SM_BYTES / (buf + tables + RING_STATIC), two = SM_BYTES / (2 * buf + tables + RING_STATIC);
+  if (two >= 8) return launch_ring<T, 128, 8, MODE>(logits, grad, p, M, buf, 2, tables, two, status, st);
+  if (one >= 6) return launch_ring<T, 128, 8, MODE>(logits, grad, p, M, buf, 1, tables, one, status, st);
+  if (one >= 4) return launch_ring<T, 256, 4, MODE>(logits, grad, p, M, buf, 1, tables, one, status, st);
+  if (one == 3) return launch_ring<T, 256, 3, MODE>(logits, grad, p, M, buf, 1, tables, one, status, st);
+  if (one == 2) return launch_ring<T, 256, 2, MODE>(logits, grad, p, M, buf, 1, tables, one, status, st);
+  return launch_ring<T, 512, 1, MODE>(logits, grad, p, M, buf, 1, tables, one, status, st);
 }
 
 }  // namespace
@@ -667,7 +684,7 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
   cudaError_t e = cudaSuccess;
   const size_t es = dtype_size(dt);
   p.same = ((reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(grad)) & 15u) == 0 && ((ld - ldo) * (int64_t)es) % 16 == 0;
-  const bool in_ring = (int64_t)V * es + 32 <= RING_BYTES;
+  const bool in_ring = ring_supported(V, k, es);
   p.count_here = in_ring && count && M <= COUNT_HERE;
   if (count && !p.count_here) {
     e = launch_overlapped(distill_count_kernel, dim3(1), dim3(1024), 0, st, labels, M, V, n_valid);
@@ -680,7 +697,9 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
     T* g = (T*)grad;
     if (in_ring) {
       if (!two) return ring<T, EXP_ONE>(z, g, p, M, status, st);
-      return temperature == 2.0f ? ring<T, EXP_HALF>(z, g, p, M, status, st) : ring<T, EXP_TWO>(z, g, p, M, status, st);
+      if (temperature == 2.0f) return ring<T, 2>(z, g, p, M, status, st);
+      if (temperature == 3.0f) return ring<T, 3>(z, g, p, M, status, st);
+      return temperature == 4.0f ? ring<T, 4>(z, g, p, M, status, st) : ring<T, EXP_TWO>(z, g, p, M, status, st);
     }
     const bool vec = ld % N == 0 && ldo % N == 0 && ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(grad)) & 15u) == 0;
     auto go = [&](auto kernel) -> cudaError_t { return launch_overlapped(kernel, dim3((unsigned)M), dim3(256), 0, st, z, g, p); };

@@ -429,7 +429,7 @@ def check_distill(z, idx, t, y, T, wc, wk, got, n=0):
 
 
 @pytest.mark.parametrize("dtype", DTYPES)
-@pytest.mark.parametrize("T,wc,wk", [(1.0, 0.5, 0.5), (2.0, 0.3, 0.7), (1.5, 0.0, 1.0), (4.0, 1.0, 1.0), (0.7, 0.2, 1.0), (2.0, 1.0, 0.0)])
+@pytest.mark.parametrize("T,wc,wk", [(1.0, 0.5, 0.5), (2.0, 0.3, 0.7), (1.5, 0.0, 1.0), (4.0, 1.0, 1.0), (3.0, 0.5, 0.5), (0.7, 0.2, 1.0), (2.0, 1.0, 0.0)])
 @pytest.mark.parametrize("M,V,k", [(1, 1, 1), (1, 50, 5), (7, 64, 64), (9, 1000, 8), (12, 1001, 33), (64, 1024, 256), (10, 32000, 20), (8, 50257, 64), (3, 30, 100)])
 def test_distill_loss(M, V, k, dtype, T, wc, wk):
     z, idx, t, y = distill_case(M, V, k, dtype, M + V + k)
