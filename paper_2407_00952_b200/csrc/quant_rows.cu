@@ -23,6 +23,7 @@ namespace {
 
 constexpr float TINY_ROW = 1e-36f;       // below this 127 / max overflows: the row is held as zero
 constexpr int NV = 4;                    // accesses of 16 bytes per thread
+constexpr int NV_CODES = 8, NV_SCALED = 4;       // of a thread that only quantises, without and with column factors
 // Rows on 16-byte boundaries; at any place, but all arrays of activations at the same place of a 16-byte vector; at any place.
 enum { FRAME_NONE = 0, FRAME_SAME = 1, FRAME_ANY = 2 };
 
@@ -325,7 +326,7 @@ __device__ __forceinline__ void codes_out(const uint8_t* mine, int8_t* cr, int s
   if (at.n <= 32) __syncwarp();            // before the next row's codes (whole warps: its reduction's barrier)
 }
 // Shared memory of a row's codes, for `threads` threads.
-template <typename T> __host__ __device__ constexpr int code_bytes(int threads) { return (threads * NV * Vec16<T>::N + 4 * Vec16<T>::N + 31) / 16 * 16; }
+template <typename T> __host__ __device__ constexpr int code_bytes(int threads, int nv = NV) { return (threads * nv * Vec16<T>::N + 4 * Vec16<T>::N + 31) / 16 * 16; }
 __device__ __forceinline__ uint8_t one_code(float v, const RowScale& rs) { return rs.live ? (uint8_t)code_bits(v, rs.inv) : (uint8_t)0; }
 
 // The rows of a thread: its group's, every (groups of the grid)-th (most kernels are launched with a group for every row).  `lead`: the row of the block's first group, by which all its
@@ -340,65 +341,69 @@ struct Walk {
   }
 };
 
-template <typename T, int FRAME>
+// COL: with column factors, whose products stay in registers, for which a thread takes fewer accesses (factors read twice were 32 bytes
+// each time for 16 of x: 4096 x 11008 bf16 40 us).
+template <typename T, int FRAME, bool COL>
 __global__ void __launch_bounds__(1024)
 quantize_kernel(const T* __restrict__ x, const float* __restrict__ factor, int64_t M, int d, int threads, int8_t* __restrict__ codes, int64_t ldc,
                 int words, float* __restrict__ scales) {
   overlap_sync();
-  constexpr int W = Vec16<T>::N;
+  constexpr int W = Vec16<T>::N, NV = COL ? NV_SCALED : NV_CODES;
   extern __shared__ __align__(16) uint8_t smem[];        // FRAME: codes
-  __shared__ RowShared sh[2];
+  __shared__ RowShared sh;
   const Place at(threads);
-  Feed<T, FRAME, 1, false> feed(0, smem);
-  feed.array(0, x);
-  uint8_t* mine = smem + (size_t)at.group * code_bytes<T>(at.n);
-  Walk w(at);
-  feed.start(w.row, M, d, at);
-  for (int flip = 0; w.lead < M; w.row += w.step, w.lead += w.step, flip ^= 1) {
-    const bool in = w.row < M;             // lanes of a row past the last still take part in the warp's exchanges
-    const T* xr = x + (in ? w.row : 0) * d;
-    const Span<T, FRAME> f(xr, d);
-    const int v1 = in ? f.v1 : 0;
-    const bool has_edge = FRAME && in && at.t < f.edges;
-    feed.begin(w.row, w.row + w.step, M, d, at);
-    float top = 0.f;
+  const bool in = at.row < M;              // lanes of a row past the last still take part in the warp's exchanges
+  const T* xr = x + (in ? at.row : 0) * d;
+  const Span<T, FRAME> f(xr, d);
+  const int v1 = in ? f.v1 : 0;
+  Vec16<T> raw[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int v = f.v0 + k * at.n + at.t;
-      if (v < v1) {
-        const Pairs<T> o = scaled<T, FRAME>(feed.raw[0][k], factor, f, v);
+  for (int k = 0; k < NV; ++k) {           // everything the row needs is under way before the first use
+    const int v = f.v0 + k * at.n + at.t;
+    if (v < v1) raw[k].load(xr + f.column(v));
+  }
+  const bool has_edge = FRAME && in && at.t < f.edges;
+  const int ec = f.edge(at.t);
+  float top = 0.f, ev = 0.f;
+  if (has_edge) {
+    ev = to_f<T>(xr[ec]);
+    if (COL) ev = __fmul_rn(ev, factor[ec]);
+    top = max_abs(top, ev);
+  }
+  Pairs<T> kept[COL ? NV : 1];
 #pragma unroll
-        for (int i = 0; i < W / 2; ++i) top = max_abs(top, o.v[i]);
-      }
-    }
-    float ev = 0.f;
-    if (has_edge) {
-      ev = to_f<T>(feed.edge[0]);
-      if (factor) ev = __fmul_rn(ev, factor[f.edge(at.t)]);
-      top = max_abs(top, ev);
-    }
-    reduce_row<0, true>(nullptr, top, at, &sh[flip]);
-    const RowScale rs = row_scale(top, 1.0f);
-    if (at.t == 0 && in) scales[w.row] = rs.scale;
-    int8_t* cr = codes + w.row * ldc;
+  for (int k = 0; k < NV; ++k) {
+    const int v = f.v0 + k * at.n + at.t;
+    if (v < v1) {
+      Pairs<T>& o = kept[COL ? k : 0];
+      if constexpr (COL) o = scaled<T, FRAME>(raw[k], factor, f, v);
+      else o = pairs_of(raw[k]);
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int v = f.v0 + k * at.n + at.t;
-      if (v < v1) {
-        uint32_t q[W / 4];
-        code_words<T>(q, scaled<T, FRAME>(feed.raw[0][k], factor, f, v), rs.inv, rs.live);
-        store_words<W>(FRAME ? (void*)(mine + v * W) : (void*)(cr + v * W), q);
-      }
+      for (int i = 0; i < W / 2; ++i) top = max_abs(top, o.v[i]);
     }
-    if constexpr (FRAME) {
-      if (has_edge) mine[f.s + f.edge(at.t)] = one_code(ev, rs);
-      codes_out(mine, cr, f.s, in ? d : 0, at, words != 0);
+  }
+  reduce_row<0, true>(nullptr, top, at, &sh);
+  const RowScale rs = row_scale(top, 1.0f);
+  if (at.t == 0 && in) scales[at.row] = rs.scale;
+  int8_t* cr = codes + at.row * ldc;
+  uint8_t* mine = FRAME ? smem + (size_t)at.group * code_bytes<T>(at.n, NV) : nullptr;
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = f.v0 + k * at.n + at.t;
+    if (v < v1) {
+      uint32_t q[W / 4];
+      if constexpr (COL) code_words<T>(q, kept[k], rs.inv, rs.live);
+      else code_words<T>(q, pairs_of(raw[k]), rs.inv, rs.live);
+      store_words<W>(FRAME ? (void*)(mine + v * W) : (void*)(cr + v * W), q);
     }
-    feed.end(w.row + w.step, M, d, at);
+  }
+  if constexpr (FRAME) {
+    if (has_edge) mine[f.s + ec] = one_code(ev, rs);
+    codes_out(mine, cr, f.s, in ? d : 0, at, words != 0);
   }
 }
 
-// Rows wider than the registers of 1024 threads hold: read twice, the second time from L2.
+// Rows wider than the registers of 1024 threads (FRAME: 48 KB of codes) hold: read twice, the second time from L2.
 template <typename T, int FRAME>
 __global__ void __launch_bounds__(1024)
 quantize_wide_kernel(const T* __restrict__ x, const float* __restrict__ factor, int d, int8_t* __restrict__ codes, int64_t ldc, float* __restrict__ scales) {
@@ -770,9 +775,9 @@ __global__ void __launch_bounds__(256) dg_reduce_kernel(const float* __restrict_
 
 bool al(const void* p, int a) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(a - 1)) == 0; }
 
-// Threads per row: as many as give each NV accesses, a power of two up to a warp, else whole warps.  frame: an edge per thread.
-template <typename T> int row_threads(int d, bool frame) {
-  const int nv = (d + Vec16<T>::N - 1) / Vec16<T>::N, need = (nv + NV - 1) / NV;
+// Threads per row: as many as give each `nv_each` accesses, a power of two up to a warp, else whole warps.  frame: an edge per thread.
+template <typename T> int row_threads(int d, bool frame, int nv_each = NV) {
+  const int nv = (d + Vec16<T>::N - 1) / Vec16<T>::N, need = (nv + nv_each - 1) / nv_each;
   if (need > 32) return (need + 31) / 32 * 32;
   int n = frame ? 2 * Vec16<T>::N : 1;
   while (n < need) n *= 2;
@@ -789,12 +794,16 @@ Shape shape_of(int64_t M, int threads) {
   return s;
 }
 
-template <typename T, int FRAME>
-cudaError_t quantize_t(const T* x, const float* factor, int64_t M, int d, int threads, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+template <typename T, int FRAME, bool COL>
+cudaError_t quantize_t(const T* x, const float* factor, int64_t M, int d, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
+  constexpr int nv = COL ? NV_SCALED : NV_CODES;
+  const int threads = row_threads<T>(d, FRAME != 0, nv);
+  if (threads > 1024 || (FRAME && code_bytes<T>(threads, nv) > 48 * 1024))         // wider than registers, or shared memory, take
+    return launch_overlapped(quantize_wide_kernel<T, FRAME>, dim3((unsigned)M), dim3(1024), 0, st, x, factor, d, codes, ldc, scales);
   const Shape s = shape_of(M, threads);
   const int words = ldc % 4 == 0 && al(codes, 4);
-  return launch_overlapped(quantize_kernel<T, FRAME>, dim3((unsigned)s.blocks), dim3(s.block), FRAME ? (size_t)s.per * code_bytes<T>(threads) : 0, st, x, factor,
-                           M, d, threads, codes, ldc, words, scales);
+  return launch_overlapped(quantize_kernel<T, FRAME, COL>, dim3((unsigned)s.blocks), dim3(s.block), FRAME ? (size_t)s.per * code_bytes<T>(threads, nv) : 0, st,
+                           x, factor, M, d, threads, codes, ldc, words, scales);
 }
 template <typename T, int FRAME>
 cudaError_t norm_t(const T* x, const T* resid, const T* g, int64_t M, int d, float eps, T* h, T* y, int8_t* codes, int64_t ldc, float* scales, cudaStream_t st) {
@@ -844,12 +853,9 @@ cudaError_t quantize_rows(int dt, const void* x, const float* factor, int64_t M,
     using T = decltype(type);
     constexpr int W = Vec16<T>::N;
     const bool frame = d % W != 0 || ldc % W != 0 || !al(x, 16) || !al(factor, 16) || !al(codes, W);
-    const int threads = row_threads<T>(d, frame);
-    if (threads > 1024)
-      return launch_overlapped(frame ? quantize_wide_kernel<T, FRAME_SAME> : quantize_wide_kernel<T, FRAME_NONE>, dim3((unsigned)M), dim3(1024), 0, st, (const T*)x,
-                               factor, d, codes, ldc, scales);
-    return frame ? quantize_t<T, FRAME_SAME>((const T*)x, factor, M, d, threads, codes, ldc, scales, st)
-                 : quantize_t<T, FRAME_NONE>((const T*)x, factor, M, d, threads, codes, ldc, scales, st);
+    auto go = [&](auto launch) { return launch((const T*)x, factor, M, d, codes, ldc, scales, st); };
+    if (factor) return frame ? go(quantize_t<T, FRAME_SAME, true>) : go(quantize_t<T, FRAME_NONE, true>);
+    return frame ? go(quantize_t<T, FRAME_SAME, false>) : go(quantize_t<T, FRAME_NONE, false>);
   };
   return dt == DT_BF16 ? run(bf16()) : run(float());
 }
