@@ -74,7 +74,8 @@ def hard_rows(x):
 
 @pytest.mark.parametrize("dtype", DTYPES)
 @pytest.mark.parametrize("M,d", [(1, 1), (1, 128), (3, 7), (9, 8), (17, 100), (64, 1024), (65, 1000), (33, 1001), (5, 4096), (12, 11008), (10, 16385),
-                                 (9, 20000), (9, 65536), (9, 40001)])
+                                 (9, 20000), (9, 65536), (9, 40001), (9, 32771),
+                                 (9, 49001), (9, 60001)])
 def test_quantize_rows(M, d, dtype):
     x = hard_rows(randn(gen(M + d), M, d)).to(dtype)
     f = 0.5 + torch.rand(d, device="cuda", generator=gen(3), dtype=torch.float32)
@@ -455,6 +456,38 @@ def test_distill_loss_layouts_and_in_place(V, ld, by, dtype):
     check_distill(z, idx, t, y, 2.0, 0.5, 0.5, (got[0], got[1], got[2][:, :V]))
     same = B.distill_loss(wide, idx, t, labels=y, temperature=2.0, ce_weight=0.5, kd_weight=0.5, vocab=V, dlogits=wide)
     assert same[2].data_ptr() == wide.data_ptr() and torch.equal(wide, got[2]) and torch.equal(same[0], got[0]) and torch.equal(same[1], got[1])
+
+
+@pytest.mark.parametrize("dtype,V,ld", [(torch.bfloat16, 131072, 131072), (torch.bfloat16, 128001, 128001), (torch.float32, 60000, 60008), (torch.float32, 65537, 65537),
+                                        (torch.bfloat16, 113001, 113001), (torch.float32, 56001, 56001)])
+def test_distill_loss_of_large_vocabularies(dtype, V, ld):
+    """Rows about as wide as shared memory, and wider."""
+    z, idx, t, y = distill_case(7, V, 40, dtype, V)
+    wide = torch.full((7, ld), 50.0, dtype=dtype, device="cuda")
+    wide[:, :V] = z
+    for T in (1.0, 2.0, 1.5):
+        got = B.distill_loss(wide, idx, t, labels=y, temperature=T, ce_weight=0.5, kd_weight=0.5, vocab=V)
+        assert (got[2][:, V:] == 0).all()
+        check_distill(z, idx, t, y, T, 0.5, 0.5, (got[0], got[1], got[2][:, :V]))
+        same = wide.clone()
+        again = B.distill_loss(same, idx, t, labels=y, temperature=T, ce_weight=0.5, kd_weight=0.5, vocab=V, dlogits=same)
+        assert torch.equal(same, got[2]) and torch.equal(again[1], got[1])
+
+
+@pytest.mark.parametrize("M", [300, 5000])
+def test_distill_loss_of_many_rows(M):
+    """More rows than blocks, and than a block looks at together; many that take no part, first and last among them."""
+    g = gen(M)
+    z = (2 * randn(g, M, 201)).to(torch.bfloat16)
+    idx = torch.randint(-3, 201, (M, 6), device="cuda", generator=g, dtype=torch.int32)
+    t = randn(g, M, 6)
+    y = torch.randint(0, 201, (M,), device="cuda", generator=g, dtype=torch.int32)
+    y[torch.rand(M, device="cuda", generator=g, dtype=torch.float32) < 0.6] = -1
+    y[0] = y[-1] = -1
+    check_distill(z, idx, t, y, 2.0, 0.5, 0.5, B.distill_loss(z, idx, t, labels=y, temperature=2.0, ce_weight=0.5, kd_weight=0.5))
+    y[:] = -1
+    y[M // 2] = 200
+    check_distill(z, idx, t, y, 1.7, 0.5, 0.5, B.distill_loss(z, idx, t, labels=y, temperature=1.7, ce_weight=0.5, kd_weight=0.5))
 
 
 def test_distill_loss_normalizer_and_no_rows():
