@@ -267,10 +267,10 @@ int splitlora_aggregate_broadcast(splitlora_ctx* ctx);
 int splitlora_loss_device(splitlora_ctx* ctx, const float** loss_dev);
 
 const char* splitlora_last_error(const splitlora_ctx* ctx);
-/* The stand-alone operators below that take no status word (attention, the LoRA linear layer) record an
- * expired bounded wait in a word the library keeps per device.  This call synchronises the current device, copies that word to *code (HOST) and
- * returns SPLITLORA_ERR_TIMEOUT when it is non-zero, else SPLITLORA_OK.  The kernels of a context
- * report through splitlora_device_status instead. */
+/* The stand-alone operators below that take no status word (attention, the LoRA linear layer, products of codes, the loss
+ * against a teacher) record an expired bounded wait in a word the library keeps per device.  This call synchronises the
+ * current device, copies that word to *code (HOST) and returns SPLITLORA_ERR_TIMEOUT when it is non-zero, else
+ * SPLITLORA_OK.  The kernels of a context report through splitlora_device_status instead. */
 int splitlora_library_status(int32_t* code);
 /* Reads the device status word (HOST out): 0, or the code left by a bounded wait that expired.
  * Synchronises the stream. */
@@ -359,7 +359,9 @@ int splitlora_handoff_dequantize(int dtype, const uint8_t* codes, const float* s
  * [out, in] an output channel.  The calls below take any sizes in the limits given and any alignment of an element;
  * 16-byte aligned rows are the fast ones.  M: rows, 1 <= M < 2^31.  ld_codes, ld_x, ld_w: bytes between two rows of codes, at
  * least the row's width; multiples of 16 (with 16-byte aligned bases) let the product run on the tensor cores.  Bytes
- * between a row's codes and the next row are neither read into a result nor written.
+ * between a row's codes and the next row are neither read into a result nor written.  The calls keep no memory of their own, so two
+ * of them on different streams meet only in buffers that both are given (a workspace of the norm's backward among them).
+ * The first call of each on a device looks up addresses and sets kernel attributes: make it outside any stream capture.
  *
  * _quantize_rows: with v = x[m,c] * col_scale[c] (col_scale [d] fp32 or NULL: v = x) and a = max_c |v|, in fp32,
  *   codes[m,c] = v * (127 / a) rounded to the nearest integer, ties to even;  scales[m] = a / 127.
@@ -375,7 +377,7 @@ int splitlora_dequantize_rows(int dtype, const int8_t* codes, int64_t ld_codes, 
  *   rstd = (mean_c s^2 + eps)^-1/2 ;  v = s g ;  codes and a as above ;  scales[m] = a rstd / 127
  *   h = s (NULL: not written) and y = v rstd (NULL: not written), each rounded once to `dtype`.
  * x, residual, h, y [M, d], g [d] in `dtype`, contiguous; h may be x or residual.  1 <= d <= 16384, eps >= 0.  A row that
- * holds an inf or NaN has scale NaN and codes 0.
+ * holds an inf or NaN has scale NaN and codes 0; where sum s^2 passes fp32's range rstd is 0, and with it scale and y.
  * _bwd: the gradient with respect to s (which is that of x and of residual) from dy, the gradient of the normalised row (the rounding
  * to codes passes it on unchanged), and h as stored:
  *   w = dy g ;  dx = residual + rstd (w - h rstd^2 mean_c(w h)) ;  dg_c = sum_m dy h rstd
@@ -388,7 +390,8 @@ int splitlora_rmsnorm_bwd(int dtype, const void* dy, const void* h, const void* 
                           int64_t M, int d, void* dx, float* dg, void* workspace, size_t workspace_bytes, void* stream);
 /* Linear layer over codes:  y[m,n] = (sum_k x[m,k] W[n,k]) * (x_scales[m] w_scales[n]) + bias[n] + residual[m,n]
  * x [M, in] and W [out, in] int8, x_scales [M], w_scales [out] or NULL (ones) fp32; bias [out] or NULL, residual [M, out] or NULL
- * and y [M, out] in `dtype`, contiguous.  The sum is exact in 32 bits (1 <= in <= 65536), the rest fp32, rounded once.  residual also
+ * and y [M, out] in `dtype`, contiguous.  The sum is exact in 32 bits (1 <= in <= 65536; M, out <= 2^30 and
+ * at most 2^28 tiles of 64 x 64), the rest fp32, rounded once.  residual also
  * takes the rank-r term of an adapter.  y may be residual.  Reports an expired wait to the library's status word. */
 int splitlora_linear_i8(int dtype, const int8_t* x, int64_t ld_x, const float* x_scales, const int8_t* W, int64_t ld_w,
                         const float* w_scales, const void* bias, const void* residual, int M, int n_in, int n_out, void* y,
@@ -404,7 +407,7 @@ int splitlora_linear_i8(int dtype, const int8_t* x, int64_t ld_x, const float* x
  * index that occurs twice counts twice.  -inf logits have probability 0; a row with a NaN or +inf logit, or with none above
  * -inf, becomes NaN.
  * logits [M, ld] and dlogits [M, ld_grad] in `dtype` (the same buffer, with the same ld, or buffers that do not
- * overlap); columns [vocab, ld_grad) of dlogits become zero.  top_idx int32 and top_logits fp32 [M, k], 1 <= k <= 256;
+ * overlap); columns [vocab, ld_grad) of dlogits become zero; M, ld, ld_grad <= 2^30.  top_idx int32 and top_logits fp32 [M, k], 1 <= k <= 256;
  * 1e-3 <= T <= 1e3; row_loss [M], loss [1], n_valid [1] (scratch) on the device.  Nothing is returned to the host. */
 int splitlora_distill_loss(int dtype, const void* logits, int64_t ld, const int32_t* labels, const int32_t* top_idx,
                            const float* top_logits, int M, int vocab, int k, float temperature, float ce_weight,

@@ -15,6 +15,8 @@ namespace {
 bool aligned(const void* p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 bool dtype_ok(int dt) { return dt == DT_F32 || dt == DT_BF16; }
 bool aligned_elem(int dt, const void* p) { return aligned(p, dt == DT_BF16 ? 2 : 4); }
+// Where a side of a matrix is indexed in 32 bits: tiles and strides past its end stay inside them.
+constexpr int64_t SIDE_MOST = 1 << 30;
 bool rows_ok(int64_t M) { return M >= 1 && M <= 2147483647LL; }
 int done(cudaError_t e) { return e == cudaSuccess ? SPLITLORA_OK : SPLITLORA_ERR_CUDA; }
 }  // namespace
@@ -69,7 +71,8 @@ int splitlora_rmsnorm_bwd(int dtype, const void* dy, const void* h, const void* 
 int splitlora_linear_i8(int dtype, const int8_t* x, int64_t ld_x, const float* x_scales, const int8_t* W, int64_t ld_w, const float* w_scales,
                         const void* bias, const void* residual, int M, int n_in, int n_out, void* y, void* stream) {
   LaunchChain chain;
-  if (!dtype_ok(dtype) || !x || !x_scales || !W || !y || M < 1 || n_in < 1 || n_in > QUANT_MAX_WIDTH || n_out < 1 || ld_x < n_in || ld_w < n_in)
+  if (!dtype_ok(dtype) || !x || !x_scales || !W || !y || M < 1 || M > SIDE_MOST || n_in < 1 || n_in > QUANT_MAX_WIDTH || n_out < 1 ||
+      n_out > SIDE_MOST || ld_x < n_in || ld_w < n_in)
     return SPLITLORA_ERR_ARG;
   if ((int64_t)((M + 63) / 64) * ((n_out + 63) / 64) > (1 << 28)) return SPLITLORA_ERR_ARG;
   if (!aligned(x_scales, 4) || !aligned(w_scales, 4)) return SPLITLORA_ERR_ALIGN;
@@ -87,8 +90,8 @@ int splitlora_distill_loss(int dtype, const void* logits, int64_t ld, const int3
                            int vocab, int k, float temperature, float ce_weight, float kd_weight, int64_t normalizer, void* dlogits, int64_t ld_grad,
                            float* row_loss, float* loss, int32_t* n_valid, void* stream) {
   LaunchChain chain;
-  if (!dtype_ok(dtype) || !logits || !top_idx || !top_logits || !dlogits || !row_loss || !loss || !n_valid || M < 1 || vocab < 1 || k < 1 ||
-      k > DISTILL_MAX_K || ld < vocab || ld_grad < vocab || normalizer < 0 || normalizer > 2147483647LL)
+  if (!dtype_ok(dtype) || !logits || !top_idx || !top_logits || !dlogits || !row_loss || !loss || !n_valid || M < 1 || M > SIDE_MOST || vocab < 1 ||
+      k < 1 || k > DISTILL_MAX_K || ld < vocab || ld > SIDE_MOST || ld_grad < vocab || ld_grad > SIDE_MOST || normalizer < 0 || normalizer > 2147483647LL)
     return SPLITLORA_ERR_ARG;
   if (!(temperature >= 1e-3f) || !(temperature <= 1e3f) || !std::isfinite(ce_weight) || !std::isfinite(kd_weight)) return SPLITLORA_ERR_ARG;
   if (!labels && ce_weight != 0.f) return SPLITLORA_ERR_ARG;

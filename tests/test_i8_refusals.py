@@ -100,6 +100,17 @@ def test_distill_refuses(bad, code):
     assert distill(**bad) == code
 
 
+@pytest.mark.parametrize("bad", [dict(M=2147483647, K=1, N=1), dict(M=5, K=1, N=2147483647), dict(M=(1 << 30) + 1, N=8), dict(M=8, N=(1 << 30) + 1)])
+def test_linear_refuses_sizes_whose_tiles_pass_32_bits(bad):
+    assert linear(**bad) == ARG
+
+
+@pytest.mark.parametrize("bad", [dict(M=2147483647, V=1, ld=1, ldg=1), dict(M=(1 << 30) + 1), dict(M=1, V=(1 << 30) + 1, ld=1 << 31, ldg=1 << 31),
+                                 dict(M=1, ldg=(1 << 30) + 1), dict(M=1, ldg=1 << 33), dict(M=1, ld=1 << 33)])
+def test_distill_refuses_sizes_whose_indexes_pass_32_bits(bad):
+    assert distill(**bad) == ARG
+
+
 def test_binding_refuses_tensors_off_the_device():
     import torch
     if torch.cuda.is_available():
