@@ -378,6 +378,7 @@ int splitlora_dequantize_rows(int dtype, const int8_t* codes, int64_t ld_codes, 
  *   h = s (NULL: not written) and y = v rstd (NULL: not written), each rounded once to `dtype`.
  * x, residual, h, y [M, d], g [d] in `dtype`, contiguous; h may be x or residual.  1 <= d <= 16384, eps >= 0.  A row that
  * holds an inf or NaN has scale NaN and codes 0; where sum s^2 passes fp32's range rstd is 0, and with it scale and y.
+ * The codes do not depend on where the rows lie; rstd may in its last bits, since the order of a row's sum follows its 16-byte vectors.
  * _bwd: the gradient with respect to s (which is that of x and of residual) from dy, the gradient of the normalised row (the rounding
  * to codes passes it on unchanged), and h as stored:
  *   w = dy g ;  dx = residual + rstd (w - h rstd^2 mean_c(w h)) ;  dg_c = sum_m dy h rstd

@@ -3,11 +3,14 @@
 //   q = softmax_j(t_j / T) over the row's entries,  p1 = softmax(z),  pT = softmax(z / T)
 //   row  = wc (-log p1[y])  +  wk T^2 sum_j q_j (log q_j - log pT[idx_j])
 //   dz_v = ( wc (p1_v - [v = y])  +  wk T (pT_v - sum_{j: idx_j = v} q_j) ) / n
-// Both softmaxes share the row's maximum.  One block per row: a pass for the maximum and the sums of exponentials (running, so
-// the logits are read once for it), a pass that writes the gradient from the logits' second read (L1 or L2), then the at most
-// k + 1 entries that carry a target are written again from their saved logits, with all of a repeated index's weights summed by
-// the first of its entries in order: one rounding per output, no atomics.  Exponents are formed as (z - max) * log2(e) / T: for
-// the entries that matter z - max is small, so the fp32 rounding of the product stays near 2^-24 of the probability.
+// Both softmaxes share the row's maximum.  Rows that fit in shared memory (114 thousand bf16 logits, 57 thousand fp32) are held there
+// between their one read and one write (distill_ring_kernel), wider ones are read twice (distill_kernel).  In both the at most k + 1
+// entries that carry a target are written again from their saved logits, with all of a repeated index's weights summed by the first
+// of its entries in order: one rounding per output, no atomics.  Exponents are formed as (z - max) * log2(e) / T: for the entries
+// that matter z - max is small, so the fp32 rounding of the product stays near 2^-24 of the probability.
+// 4096 x 50257 bf16, k = 32, both terms: 174 us at T = 2, 179 at T = 4, 261 at T = 1.3; the traffic alone takes 126.
+// The gradient may be written over the logits: every element is read before it is written, and written by the thread that read it or
+// behind a barrier.
 #include "common.cuh"
 #include "host_common.h"
 #include "kernels.h"
@@ -52,9 +55,12 @@ template <int MODE> __device__ __forceinline__ void online_merge(Online& a, cons
   a.m = m;
 }
 
+// Rows wider than shared memory, one block each: a pass for the maximum and the running sums of exponentials, a pass that writes the
+// gradient from the logits' second read (L1 or L2).  4 exponentials per logit with two temperatures: bound by the exponential unit and
+// instruction issue as much as by traffic (it took 467 us where the ring kernel takes 174).
 template <typename T, int W, int MODE>
 __global__ void __launch_bounds__(512)
-distill_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p) {   // grad may be logits
+distill_kernel(const T* logits, T* grad, DistillArgs p) {
   overlap_sync();
   __shared__ Online sh_on[16];
   __shared__ float sh_red[16];
@@ -234,10 +240,10 @@ distill_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p
 // rows in shared memory
 // ------------------------------------------------------------------------------------------
 // Persistent blocks walk the rows.  One thread copies the next rows into a ring of one or two buffers with bulk copies; a row's
-// logits are read from there twice (maximum, exponentials), the exponentials of a temperature stay in registers until the
-// row's sums are known, and the gradient leaves from there: a logit costs HBM one read and one write, and one exponential where
-// one temperature is enough or the two are 1 and 2, 3 or 4 (then e^z = (e^(z/2))^2 and so on).  What bounds the streaming kernel above is the
-// exponential unit and instruction issue (4 exponentials per logit) as much as traffic.
+// logits are read from there three times (maximum, sums, gradient; keeping the exponentials in registers between the last two took 280 us
+// where this takes 174: fewer rows per SM), and the gradient leaves from there: a logit costs HBM one read and one write, and
+// two exponentials where one temperature is enough or the two are 1 and 2, 3 or 4 (then e^z = (e^(z/2))^2 and so on), else four.
+// Bounded by shared memory's reads, issue and HBM alike; fp32, twice the bytes for the same exponentials, by HBM.
 // Rows may start anywhere (a vocabulary of 50257 entries in contiguous rows): a row is held as the 16-byte vectors that cover it, its
 // first and last vector patched by the threads that own them; the copies take whole vectors inside the buffer and plain
 // loads the ragged ends of the first and last row.
@@ -277,7 +283,7 @@ constexpr int BATCH = 128;   // rows of a block that are looked at together for 
 // warps: 0 the row's loss, 1 the ragged ends and the teacher's distribution of the next row, the others the previous row's targets.
 template <typename T, int THREADS, int MINB, int MODE>
 __global__ void __launch_bounds__(THREADS, MINB)
-distill_ring_kernel(const T* __restrict__ logits, T* __restrict__ grad, DistillArgs p, int M, int nbuf, int buf_bytes, int* status) {
+distill_ring_kernel(const T* logits, T* grad, DistillArgs p, int M, int nbuf, int buf_bytes, int* status) {
   constexpr int W = Vec16<T>::N, NW = THREADS / 32, ISSUER = THREADS - 32;
   constexpr int UNROLL = THREADS > 128 ? 4 : 2;          // many blocks in different places of their rows: the code has to stay cached
   extern __shared__ __align__(128) uint8_t smem[];       // nbuf rows, then the tables of the teacher's entries
@@ -633,7 +639,7 @@ namespace {
 // Rows up to this many labels are counted by every block of the ring kernel instead of a launch in front of it.
 constexpr int COUNT_HERE = 4096;
 // Static shared memory of a block with what the system keeps per block, dynamic shared memory of a block, all of an SM's.
-constexpr int RING_STATIC = 4096, RING_BYTES = 232448 - 3072, SM_BYTES = 233472;
+constexpr int RING_STATIC = 4096, RING_BYTES = 229376, SM_BYTES = 233472;
 
 template <typename T, int THREADS, int MINB, int MODE>
 cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, int buf, int nbuf, int tables, int fit, int* status, cudaStream_t st) {

@@ -6,9 +6,13 @@
 // The codes of a normalised row do not depend on rstd: it scales the row and its maximum alike, so one pass over the row
 // collects sum s^2 and max |s g| together and every rounding decision is one of fp32 products and one fp32 division, whatever
 // the order of the sum.  All arithmetic is fp32; h and y are rounded once to the buffers' type, the norm sees s before that.
-// Bounded by HBM: a row lives in registers between its reduction and its output (4 accesses of 16 bytes per thread; 1 to 32 lanes
-// per row up to 128 accesses, else whole warps, up to 1024 threads), so it is read once.  Rows are many and short-lived: a block
-// each (walking the rows with copies one row ahead was 10-20 % slower where no sums are carried from row to row). 
+// Bounded by HBM: a row lives in registers between its reduction and its output (4 or 8 accesses of 16 bytes per thread; 1 to 32
+// lanes per row where a warp holds it, else whole warps, up to 1024 threads), so it is read once.  Rows are many and short-lived: a
+// block each (walking the rows with copies one row ahead was 10-20 % slower where no sums are carried from row to row).
+// 8192 x 4096 bf16, and the time of the traffic alone at the chip's measured copy rate: quantize 18.6 us (15.4), dequantize 16.5
+// (15.4), norm with residual, h and codes 42.5 (35.9), with y too 51 (46.2), gradient 38.6 (30.8), with residual 50 (41.1), with
+// residual and gain gradient 67 (41.1).
+// An output may be one of the inputs where the call allows it: a thread writes only elements that it alone has read.
 // FRAME: rows that do not start on 16-byte boundaries (odd widths in contiguous rows).  A row is then the whole 16-byte vectors in
 // it, position q = column + shift, and the elements around them, which are taken one by one; the gain and the factors, which start
 // at column 0, are read as words and shifted, and the codes turn back to column 0 through shared memory.
@@ -329,8 +333,8 @@ __device__ __forceinline__ void codes_out(const uint8_t* mine, int8_t* cr, int s
 template <typename T> __host__ __device__ constexpr int code_bytes(int threads, int nv = NV) { return (threads * nv * Vec16<T>::N + 4 * Vec16<T>::N + 31) / 16 * 16; }
 __device__ __forceinline__ uint8_t one_code(float v, const RowScale& rs) { return rs.live ? (uint8_t)code_bits(v, rs.inv) : (uint8_t)0; }
 
-// The rows of a thread: its group's, every (groups of the grid)-th (most kernels are launched with a group for every row).  `lead`: the row of the block's first group, by which all its
-// threads go through the same number of rows.
+// The rows of a thread: its group's, every (groups of the grid)-th; only the gain's gradient is launched with fewer groups than
+// rows.  `lead`: the row of the block's first group, by which all its threads go through the same number of rows.
 struct Walk {
   int64_t row, lead, step;
   __device__ __forceinline__ explicit Walk(const Place& at) {
@@ -341,8 +345,8 @@ struct Walk {
   }
 };
 
-// COL: with column factors, whose products stay in registers, for which a thread takes fewer accesses (factors read twice were 32 bytes
-// each time for 16 of x: 4096 x 11008 bf16 40 us).
+// COL: with column factors, whose products stay in registers, for which a thread takes fewer accesses (4096 x 11008 bf16 41 us, 25
+// without factors; 8192 x 4096 24.7 and 18.6.  Four accesses per thread without factors: 35 and 24.7).
 template <typename T, int FRAME, bool COL>
 __global__ void __launch_bounds__(1024)
 quantize_kernel(const T* __restrict__ x, const float* __restrict__ factor, int64_t M, int d, int threads, int8_t* __restrict__ codes, int64_t ldc,

@@ -638,3 +638,58 @@ def test_refusals_on_the_device():
         with pytest.raises(B.SplitLoraError) as e:
             f()
         assert e.value.code == -1
+
+
+def test_element_offsets_beyond_32_bits():
+    """More than 2^31 elements: the last rows come out as they do by themselves, bit for bit, and the first rows with them."""
+    def ends(n, k=40):
+        return [slice(0, k), slice(n - k, n)]
+
+    g = gen(5)
+    M, d = 33001, 65536
+    x = torch.empty(M, d, dtype=torch.bfloat16, device="cuda")
+    for part in ends(M):
+        x[part] = randn(g, 40, d).to(torch.bfloat16)
+    codes, scales = B.quantize_rows(x)
+    back = B.dequantize_rows(codes, scales, out=x.clone())
+    for part in ends(M):
+        c, s = B.quantize_rows(x[part])
+        assert torch.equal(codes[part], c) and torch.equal(scales[part], s) and torch.equal(back[part], B.dequantize_rows(c, s))
+    del codes, scales, back, x
+    M, d = 131300, 16383
+    x = torch.zeros(M, d, dtype=torch.bfloat16, device="cuda")
+    r = torch.zeros_like(x)
+    gain = randn(g, d).to(torch.bfloat16)
+    for part in ends(M):
+        x[part] = randn(g, 40, d).to(torch.bfloat16)
+        r[part] = randn(g, 40, d).to(torch.bfloat16)
+    codes, scales, h, y = B.rmsnorm_quantize(x, gain, residual=r, want_y=True)
+    dx, _ = B.rmsnorm_bwd(y, h, gain, resid=x)
+    dx2, dg = B.rmsnorm_bwd(y, h, gain, resid=x, want_dg=True)
+    assert torch.equal(dx, dx2)
+    for part in ends(M):
+        # (the rows where they lie: the order of a row's sum follows its place in the 16-byte vectors)
+        c, s, h1, y1 = B.rmsnorm_quantize(x[part], gain, residual=r[part], want_y=True)
+        assert torch.equal(codes[part], c) and torch.equal(scales[part], s) and torch.equal(h[part], h1) and torch.equal(y[part], y1)
+        assert torch.equal(dx[part], B.rmsnorm_bwd(y[part], h[part], gain, resid=x[part])[0])
+    del codes, scales, h, y, dx, dx2, r, x
+    M, K, N = 70001, 64, 32768
+    a = torch.randint(-127, 128, (M, K), device="cuda", generator=g, dtype=torch.int8)
+    w = torch.randint(-127, 128, (N, K), device="cuda", generator=g, dtype=torch.int8)
+    sa, sw = randn(g, M).abs(), randn(g, N).abs()
+    for dtype in (torch.bfloat16, torch.float32):
+        res = torch.ones(M, N, dtype=dtype, device="cuda")
+        out = B.linear_i8(a, sa, w, sw, residual=res, y=res)
+        for part in ends(M):
+            assert torch.equal(out[part], B.linear_i8(a[part], sa[part], w, sw, residual=torch.ones(40, N, dtype=dtype, device="cuda"), dtype=dtype))
+        del res, out
+    M, V = 42801, 50257
+    z = torch.zeros(M, V, dtype=torch.bfloat16, device="cuda")
+    idx = torch.randint(0, V, (M, 8), device="cuda", generator=g, dtype=torch.int32)
+    t, lab = randn(g, M, 8), torch.randint(0, V, (M,), device="cuda", generator=g, dtype=torch.int32)
+    for part in ends(M):
+        z[part] = (2 * randn(g, 40, V)).to(torch.bfloat16)
+    want = [B.distill_loss(z[part].clone(), idx[part], t[part], labels=lab[part], temperature=2.0, ce_weight=0.5, kd_weight=0.5, normalizer=M) for part in ends(M)]
+    _, rows, dz = B.distill_loss(z, idx, t, labels=lab, temperature=2.0, ce_weight=0.5, kd_weight=0.5, dlogits=z)
+    for part, (_, rows1, dz1) in zip(ends(M), want):
+        assert torch.equal(rows[part], rows1) and torch.equal(dz[part], dz1)
