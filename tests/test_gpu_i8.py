@@ -474,6 +474,41 @@ def test_distill_loss_of_large_vocabularies(dtype, V, ld):
         assert torch.equal(same, got[2]) and torch.equal(again[1], got[1])
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [1.0, 1.3, 2.0, 3.0, 4.0])
+@pytest.mark.parametrize("V", [64, 1003, 20000])
+def test_distill_loss_of_masked_and_broken_logits_at_every_column(V, T, dtype):
+    """-inf logits have probability 0 exactly, wherever in a vector they stand; NaN and inf reach their own row and no other."""
+    z, idx, t, y = distill_case(40, V, 6, dtype, V + 1)
+    z, idx, t = z.clamp(min=-20), idx.clamp(0, V - 1), torch.zeros_like(t)
+    y[:] = 5
+    dead = torch.zeros(40, V, dtype=torch.bool, device="cuda")
+    for m in range(16):
+        dead[m, m::16] = True
+    for m in range(16, 20):
+        dead[m, m - 16::2] = True
+    keep = torch.zeros_like(dead).scatter_(1, idx.long(), True)
+    keep[:, 5] = True
+    dead &= ~keep
+    z[dead] = -float("inf")
+    for m in range(20, 28):
+        z[m, m] = float("nan")
+    for m in range(28, 36):
+        z[m, m] = float("inf")
+    _, rows, dz = B.distill_loss(z, idx, t, labels=y, temperature=T, ce_weight=0.5, kd_weight=0.5)
+    assert (dz[dead] == 0).all()
+    broken = torch.zeros(40, dtype=torch.bool, device="cuda")
+    broken[20:36] = True
+    assert torch.isnan(rows[broken]).all() and torch.isnan(dz[broken]).any(dim=1).all()
+    ok = ~broken
+    zz = z[ok].double().clamp(min=-1e30)
+    # rows with whatever is masked left at a logit of no weight: 64-bit formulas, tolerance as above with the finite logits' spread
+    rr, _, rg, size = distill64(zz, idx[ok], t[ok], y[ok], T, 0.5, 0.5, 40)
+    rel = (2 * 40 / min(T, 1.0) + V / 128 + 64) * U
+    check(dz[ok], rg, HALF[dtype] * rg.abs() + rel * size + 1e-40, "dlogits")
+    check(rows[ok], rr, rel * (rr.abs() + 0.5 + 0.5 * T * T * 50), "rows")
+
+
 @pytest.mark.parametrize("M", [300, 5000])
 def test_distill_loss_of_many_rows(M):
     """More rows than blocks, and than a block looks at together; many that take no part, first and last among them."""
