@@ -3,14 +3,16 @@
 //   q = softmax_j(t_j / T) over the row's entries,  p1 = softmax(z),  pT = softmax(z / T)
 //   row  = wc (-log p1[y])  +  wk T^2 sum_j q_j (log q_j - log pT[idx_j])
 //   dz_v = ( wc (p1_v - [v = y])  +  wk T (pT_v - sum_{j: idx_j = v} q_j) ) / n
-// Both softmaxes share the row's maximum.  Rows that fit in shared memory (114 thousand bf16 logits, 57 thousand fp32) are held there
-// between their one read and one write (distill_ring_kernel), wider ones are read twice (distill_kernel).  In both the at most k + 1
-// entries that carry a target are written again from their saved logits, with all of a repeated index's weights summed by the first
+// Both softmaxes share the row's maximum.  Between their one read and one write narrow rows are held in a warp's registers
+// (distill_warp_kernel), rows of up to 114 thousand bf16 or 57 thousand fp32 logits in shared memory (distill_ring_kernel); wider
+// ones are read twice (distill_kernel).  In all of them the at most k + 1 entries that carry a target are written again from their saved logits, with all of a repeated index's weights summed by the first
 // of its entries in order: one rounding per output, no atomics.  Exponents are formed as (z - max) * log2(e) / T: for the entries
 // that matter z - max is small, so the fp32 rounding of the product stays near 2^-24 of the probability.
-// 4096 x 50257 bf16, k = 32, both terms: 174 us at T = 2, 179 at T = 4, 228 at T = 1.3; the traffic alone takes 126.
+// 4096 x 50257 bf16, k = 32, both terms: 173 us at T = 2, 177 at T = 4, 226 at T = 1.3; the traffic alone takes 126.
 // The gradient may be written over the logits: every element is read before it is written, and written by the thread that read it or
 // behind a barrier.
+#include <type_traits>
+
 #include "common.cuh"
 #include "host_common.h"
 #include "kernels.h"
@@ -293,10 +295,103 @@ __device__ __forceinline__ uint64_t exp_pair_poly(uint64_t x) {
 // three eighths 243).
 __device__ __forceinline__ uint64_t exp_second(int i, uint64_t x) { return i % 2 == 1 ? exp_pair_poly(x) : exp_pair(x); }
 
+// A pair's share of the sums of exponentials (dd: logits less the maximum; i: its number in the vector), and its gradient
+// f1 e^(c1 dd) + fT e^(cT dd).
+template <int MODE> __device__ __forceinline__ void add_exps(uint64_t dd, int i, uint64_t cT2, uint64_t c12, uint64_t& sT2, uint64_t& s12) {
+  const uint64_t e = exp_pair(tc::mul2(dd, cT2));
+  sT2 = tc::add2(sT2, e);
+  if constexpr (MODE == 2) s12 = tc::fma2(e, e, s12);
+  if constexpr (MODE > 2) s12 = tc::add2(s12, power2<MODE>(e));
+  if constexpr (MODE == EXP_TWO) s12 = tc::add2(s12, exp_second(i, tc::mul2(dd, c12)));
+}
+template <int MODE> __device__ __forceinline__ uint64_t slopes(uint64_t dd, int i, uint64_t cT2, uint64_t c12, uint64_t f12, uint64_t fT2) {
+  const uint64_t e = exp_pair(tc::mul2(dd, cT2));
+  if constexpr (MODE == EXP_ONE) return tc::mul2(e, f12);
+  else if constexpr (MODE == 2) return tc::mul2(e, tc::fma2(e, f12, fT2));
+  else if constexpr (MODE > 2) return tc::fma2(power2<MODE>(e), f12, tc::mul2(e, fT2));
+  else return tc::fma2(e, fT2, tc::mul2(f12, exp_second(i, tc::mul2(dd, c12))));
+}
+template <int MODE> __device__ __forceinline__ float slope(float dd, float cT, float c1, float f1, float fT) {
+  const float x = ex2(dd * cT);
+  if constexpr (MODE == EXP_ONE) return f1 * x;
+  else if constexpr (MODE == EXP_TWO) return fmaf(f1, ex2(dd * c1), fT * x);
+  else return fmaf(f1, power<MODE>(x), fT * x);
+}
+// a vector's gradient, rounded
+template <int MODE, typename T> __device__ __forceinline__ Vec16<T> slopes_of(const Vec16<T>& r, uint64_t neg2, uint64_t cT2, uint64_t c12, uint64_t f12, uint64_t fT2) {
+  Vec16<T> o;
+#pragma unroll
+  for (int i = 0; i < Vec16<T>::N / 2; ++i) {
+    float a, c;
+    tc::unpack2(slopes<MODE>(tc::add2(pair_of(r, i), neg2), i, cT2, c12, f12, fT2), a, c);
+    if constexpr (Vec16<T>::N == 8) reinterpret_cast<__nv_bfloat162*>(&o.raw)[i] = __floats2bfloat162_rn(a, c);
+    else { o.set(2 * i, a); o.set(2 * i + 1, c); }
+  }
+  return o;
+}
+
 // maximum over a warp in one instruction, on integers in the order of the floats (no NaN comes here)
 __device__ __forceinline__ float warp_max_redux(float v) {
   const int i = __float_as_int(v), o = i ^ ((i >> 31) & 0x7fffffff), m = __reduce_max_sync(0xffffffffu, o);
   return __int_as_float(m ^ ((m >> 31) & 0x7fffffff));
+}
+
+// Positions [from, to) of a row of the gradient (position 0: a 16-byte boundary of the logits) become zero; thread t of n.
+template <typename T> __device__ __forceinline__ void zero_span(T* out, int from, int to, int t, int n, bool whole) {
+  constexpr int W = Vec16<T>::N;
+  for (int v = from / W + t; v * W < to; v += n) {
+    if (whole && v * W >= from && (v + 1) * W <= to) *reinterpret_cast<uint4*>(out + (int64_t)v * W) = make_uint4(0u, 0u, 0u, 0u);
+    else
+      for (int i = 0; i < W; ++i)
+        if (v * W + i >= from && v * W + i < to) out[v * W + i] = from_f<T>(0.f);
+  }
+}
+
+// One warp: a row's teacher entries, q holding their logits: q_j = softmax(t / T) in place, log q_j = (t_j - top) / T - lts; absent entries
+// and the room up to a multiple of four get index -1.
+struct Teacher { float top, lts; bool some; };
+__device__ __forceinline__ Teacher teacher_of(int* idx, float* q, const DistillArgs& p, int lane) {
+  const int k = p.k, k4 = (k + 3) / 4 * 4;
+  float tmax = -INFINITY, tsum = 0.f;
+  for (int j = lane; j < k; j += 32) {
+    const int v = idx[j];
+    const bool ok = v >= 0 && v < p.V;
+    const float t = ok ? q[j] : -INFINITY;
+    if (!ok) { idx[j] = -1; q[j] = t; }
+    tmax = t != t || tmax != tmax ? __uint_as_float(0x7fffffffu) : fmaxf(tmax, t);
+  }
+  for (int j = k + lane; j < k4; j += 32) idx[j] = -1;
+  const bool nan = __any_sync(0xffffffffu, tmax != tmax);
+  tmax = warp_max_redux(nan ? 0.f : tmax);
+  if (nan) tmax = __uint_as_float(0x7fffffffu);
+  const bool some = tmax != -INFINITY && p.wk != 0.f;      // else the teacher says nothing about this row
+  for (int j = lane; j < k; j += 32) tsum += some ? expf((q[j] - tmax) * p.inv_t) : 0.f;
+  tsum = warp_sum(tsum);
+  for (int j = lane; j < k; j += 32) q[j] = some ? expf((q[j] - tmax) * p.inv_t) / tsum : 0.f;
+  return {tmax, logf(tsum), some};
+}
+// The entries of a row that carry a target, entries j0, j0 + step ...: the first entry of an index writes for all of them.  zt: their logits.
+struct Slope { float base, f1, fT, fq, fy; };              // gradient = slope(z) - fq sum of q - fy at the label
+template <int MODE, typename T>
+__device__ __forceinline__ void targets(T* out, const Slope& f, const DistillArgs& p, int j0, int step, const int* idx, const float* q, const float* zt, int y, float zy) {
+  const int k = p.k;
+  for (int j = j0; j <= k; j += step) {
+    const int v = j < k ? idx[j] : p.labels ? y : -1;      // entry k: the label
+    if (v < 0) continue;
+    bool first = true;
+    float sum = 0.f;
+    for (int i = 0; i < k; i += 4) {
+      const int4 w = *reinterpret_cast<const int4*>(&idx[i]);
+      if (w.x == v) { if (i < j) first = false; sum += q[i]; }
+      if (w.y == v) { if (i + 1 < j) first = false; sum += q[i + 1]; }
+      if (w.z == v) { if (i + 2 < j) first = false; sum += q[i + 2]; }
+      if (w.w == v) { if (i + 3 < j) first = false; sum += q[i + 3]; }
+    }
+    if (!first) continue;
+    float r = slope<MODE>((j < k ? zt[j] : zy) - f.base, p.cT, p.c1, f.f1, f.fT) - f.fq * sum;
+    if (p.labels && v == y) r -= f.fy;
+    out[v] = from_f<T>(r);
+  }
 }
 
 constexpr int SLOTS = 4;     // rows whose tables are in use at once: two ahead, this one, the one whose targets are being written
@@ -367,60 +462,17 @@ distill_ring_kernel(const T* logits, T* grad, DistillArgs p, int M, int nbuf, in
       cp_async4(tc::smem_u32(&sh_q(slot)[j]), p.t + (int64_t)row * k + j);
     }
   };
-  // warp 1: t -> q = softmax(t / T) over the row's entries, absent ones as index -1
   auto teacher = [&](int slot) {
     asm volatile("cp.async.wait_all;" ::: "memory");
-    float tmax = -INFINITY, tsum = 0.f;
-    for (int j = lane; j < k; j += 32) {
-      const int v = sh_idx(slot)[j];
-      const bool ok = v >= 0 && v < V;
-      const float t = ok ? sh_q(slot)[j] : -INFINITY;
-      if (!ok) { sh_idx(slot)[j] = -1; sh_q(slot)[j] = t; }
-      tmax = t != t || tmax != tmax ? __uint_as_float(0x7fffffffu) : fmaxf(tmax, t);
-    }
-    for (int j = k + lane; j < k4; j += 32) sh_idx(slot)[j] = -1;
-    const bool nan = __any_sync(0xffffffffu, tmax != tmax);
-    tmax = warp_max_redux(nan ? 0.f : tmax);
-    if (nan) tmax = __uint_as_float(0x7fffffffu);
-    const bool teach = tmax != -INFINITY && p.wk != 0.f;     // else the teacher says nothing about this row
-    for (int j = lane; j < k; j += 32) tsum += teach ? expf((sh_q(slot)[j] - tmax) * p.inv_t) : 0.f;
-    tsum = warp_sum(tsum);
-    for (int j = lane; j < k; j += 32) sh_q(slot)[j] = teach ? expf((sh_q(slot)[j] - tmax) * p.inv_t) / tsum : 0.f;
-    if (lane == 0) { sh_teach[slot] = teach; sh_tmax[slot] = tmax; sh_lts[slot] = logf(tsum); }
+    const Teacher t = teacher_of(sh_idx(slot), sh_q(slot), p, lane);
+    if (lane == 0) { sh_teach[slot] = t.some; sh_tmax[slot] = t.top; sh_lts[slot] = t.lts; }
   };
-  // from warp 2 on: the entries of a row that carry a target; the first entry of an index writes for all of them
+  // from warp 2 on
   auto write_targets = [&](int row, int y, int slot, int par) {
-    const float f1 = sh_f1[par], fT = sh_fT[par], base = sh_base[par];
-    T* out = grad + row * p.ldo;
-    for (int j = tid - 64; j <= k; j += THREADS - 64) {
-      const int v = j < k ? sh_idx(slot)[j] : p.labels ? y : -1;       // entry k: the label
-      if (v < 0) continue;
-      bool first = true;
-      float q = 0.f;
-      for (int i = 0; i < k; i += 4) {
-        const int4 w = *reinterpret_cast<const int4*>(&sh_idx(slot)[i]);
-        if (w.x == v) { if (i < j) first = false; q += sh_q(slot)[i]; }
-        if (w.y == v) { if (i + 1 < j) first = false; q += sh_q(slot)[i + 1]; }
-        if (w.z == v) { if (i + 2 < j) first = false; q += sh_q(slot)[i + 2]; }
-        if (w.w == v) { if (i + 3 < j) first = false; q += sh_q(slot)[i + 3]; }
-      }
-      if (!first) continue;
-      const float z = (j < k ? sh_z(par)[j] : sh_zy[par]) - base, x = ex2(z * p.cT);
-      float r = MODE == EXP_ONE ? f1 * x : fmaf(f1, MODE == EXP_TWO ? ex2(z * p.c1) : power<MODE>(x), fT * x);
-      r -= sh_fq[par] * q;
-      if (p.labels && v == y) r -= p.wc * inv_n;
-      out[v] = from_f<T>(r);
-    }
+    const Slope f{sh_base[par], sh_f1[par], sh_fT[par], sh_fq[par], p.wc * inv_n};
+    targets<MODE>(grad + row * p.ldo, f, p, tid - 64, THREADS - 64, sh_idx(slot), sh_q(slot), sh_z(par), y, sh_zy[par]);
   };
-  // all threads: positions [from, to) of a row of the gradient (position 0: a 16-byte boundary of the logits) become zero
-  auto zeros = [&](T* out, int from, int to) {
-    for (int v = from / W + tid; v * W < to; v += THREADS) {
-      if (p.same && v * W >= from && (v + 1) * W <= to) *reinterpret_cast<uint4*>(out + (int64_t)v * W) = make_uint4(0u, 0u, 0u, 0u);
-      else
-        for (int i = 0; i < W; ++i)
-          if (v * W + i >= from && v * W + i < to) out[v * W + i] = from_f<T>(0.f);
-    }
-  };
+  auto zeros = [&](T* out, int from, int to) { zero_span(out, from, to, tid, THREADS, p.same != 0); };
   auto shift_of = [&](int row) { return (int)((reinterpret_cast<uintptr_t>(logits + row * p.ld) & 15u) / sizeof(T)); };
 
   const uint64_t cT2 = tc::pack2(p.cT, p.cT), c12 = tc::pack2(p.c1, p.c1);
@@ -506,12 +558,7 @@ distill_ring_kernel(const T* logits, T* grad, DistillArgs p, int M, int nbuf, in
           Vec16<T> r; r.load(zs + (size_t)v * W);
 #pragma unroll
           for (int i = 0; i < W / 2; ++i) {
-            const uint64_t dd = tc::add2(pair_of(r, i), neg2);       // z - maximum
-            const uint64_t e = exp_pair(tc::mul2(dd, cT2));
-            sT2 = tc::add2(sT2, e);
-            if constexpr (MODE == 2) s12 = tc::fma2(e, e, s12);
-            if constexpr (MODE > 2) s12 = tc::add2(s12, power2<MODE>(e));
-            if constexpr (MODE == EXP_TWO) s12 = tc::add2(s12, exp_second(i, tc::mul2(dd, c12)));
+            add_exps<MODE>(tc::add2(pair_of(r, i), neg2), i, cT2, c12, sT2, s12);
           }
         }
       }
@@ -578,8 +625,7 @@ distill_ring_kernel(const T* logits, T* grad, DistillArgs p, int M, int nbuf, in
         if (lane < 2 * W) {                // the ragged ends, one logit per lane
           const int which = lane / W, i = lane % W, q = (which ? last * W : 0) + i;
           if ((which ? ragged_last : ragged_first && !(last == 0 && ragged_last)) && q >= s && q < end) {
-            const float z = to_f<T>(sh_edge[par][which][i]) - base, x = ex2(z * p.cT);
-            out[q] = from_f<T>(MODE == EXP_ONE ? f1 * x : fmaf(f1, MODE == EXP_TWO ? ex2(z * p.c1) : power<MODE>(x), fT * x));
+            out[q] = from_f<T>(slope<MODE>(to_f<T>(sh_edge[par][which][i]) - base, p.cT, p.c1, f1, fT));
           }
         }
         __syncwarp();
@@ -593,22 +639,9 @@ distill_ring_kernel(const T* logits, T* grad, DistillArgs p, int M, int nbuf, in
       const int v_to = ragged_last ? last : nvec;
 #pragma unroll UNROLL
       for (int v = tid == 0 && ragged_first ? THREADS : tid; v < v_to; v += THREADS) {
-        Vec16<T> r, o;
+        Vec16<T> r;
         r.load(zs + (size_t)v * W);
-#pragma unroll
-        for (int i = 0; i < W / 2; ++i) {
-          const uint64_t dd = tc::add2(pair_of(r, i), neg2);
-          const uint64_t e = exp_pair(tc::mul2(dd, cT2));
-          uint64_t w;
-          if constexpr (MODE == EXP_ONE) w = tc::mul2(e, f12);
-          if constexpr (MODE == 2) w = tc::mul2(e, tc::fma2(e, f12, fT2));
-          if constexpr (MODE > 2) w = tc::fma2(power2<MODE>(e), f12, tc::mul2(e, fT2));
-          if constexpr (MODE == EXP_TWO) w = tc::fma2(e, fT2, tc::mul2(f12, exp_second(i, tc::mul2(dd, c12))));
-          float a, c;
-          tc::unpack2(w, a, c);
-          if constexpr (W == 8) reinterpret_cast<__nv_bfloat162*>(&o.raw)[i] = __floats2bfloat162_rn(a, c);
-          else { o.set(2 * i, a); o.set(2 * i + 1, c); }
-        }
+        const Vec16<T> o = slopes_of<MODE>(r, neg2, cT2, c12, f12, fT2);
         if (p.same) o.store(out + (int64_t)v * W);
         else
 #pragma unroll
@@ -627,32 +660,175 @@ distill_ring_kernel(const T* logits, T* grad, DistillArgs p, int M, int nbuf, in
   }
 }
 
-__global__ void distill_count_kernel(const int32_t* __restrict__ labels, int M, int V, int* __restrict__ n_valid) {
+// ------------------------------------------------------------------------------------------
+// rows in the registers of a warp
+// ------------------------------------------------------------------------------------------
+// A warp per row of up to 32 x NVR vectors, eight rows per block: no barriers between a row's steps, and other rows' loads in flight on
+// the SM's other warps.  What bounds it is the chain of a row (the teacher's entries, three reductions, the targets), then launches: 300
+// x 117 takes 8.3 us, of which the sum over the rows' losses, a launch of its own, is 4.
+constexpr int WARP_ROWS = 8;
+template <typename T, int NVR, int MODE>
+__global__ void __launch_bounds__(32 * WARP_ROWS, NVR == 4 ? 4 : 3)
+distill_warp_kernel(const T* logits, T* grad, DistillArgs p, int M) {
+  constexpr int W = Vec16<T>::N;
+  extern __shared__ __align__(16) int warp_tables[];       // per row: indexes, weights, logits of the teacher's entries
+  __shared__ int sh_cnt[WARP_ROWS];
+  overlap_sync();
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, V = p.V, k = p.k, k4 = (k + 3) / 4 * 4;
+  const int64_t row = (int64_t)blockIdx.x * WARP_ROWS + warp;
+  const bool in = row < M;
+  const int y = in && p.labels ? p.labels[row] : 0;
+  const bool valid = in && y >= 0 && y < V;
+  const T* z = logits + (in ? row : 0) * p.ld;
+  int* idx = warp_tables + warp * 3 * k4;
+  float* q = reinterpret_cast<float*>(idx + k4), *zt = q + k4;
+  // position = column + s; whole vectors [v0, v1) and up to 14 elements around them, one per lane
+  const int s = (int)((reinterpret_cast<uintptr_t>(z) & 15u) / sizeof(T)), end = s + V, v0 = s > 0 ? 1 : 0, v1 = max(end / W, v0);
+  const int head = v0 ? min(W, end) - s : 0, edges = head + max(end - v1 * W, 0), ec = lane < head ? lane : v1 * W - s + lane - head;
+  const bool has_edge = valid && lane < edges;
+  Vec16<T> raw[NVR];
+#pragma unroll
+  for (int i = 0; i < NVR; ++i) {
+    const int v = v0 + i * 32 + lane;
+    if (valid && v < v1) raw[i].load(z + v * W - s);
+    else
+#pragma unroll
+      for (int c = 0; c < W; ++c) raw[i].set(c, -INFINITY);
+  }
+  const float ez = has_edge ? to_f<T>(z[ec]) : -INFINITY, zy = valid && p.labels ? to_f<T>(z[y]) : 0.f;
+  if (valid)
+    for (int j = lane; j < k; j += 32) {
+      const int v = p.idx[row * k + j];
+      idx[j] = v;
+      q[j] = p.t[row * k + j];
+      zt[j] = v >= 0 && v < V ? to_f<T>(z[v]) : 0.f;
+    }
+  int n = p.n_fixed;
+  if (p.n_valid && !p.count_here) n = *p.n_valid;
+  if (p.count_here) {
+    int c = 0;
+    for (int i = tid; i < M; i += 32 * WARP_ROWS) c += p.labels[i] >= 0 && p.labels[i] < V ? 1 : 0;
+    c = __reduce_add_sync(0xffffffffu, c);
+    if (lane == 0) sh_cnt[warp] = c;
+    __syncthreads();
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < WARP_ROWS; ++w) n += sh_cnt[w];
+    if (blockIdx.x == 0 && tid == 0) *p.n_valid = n;
+  }
+  if (!in) return;
+  const float inv_n = 1.0f / (float)(n > 0 ? n : 1);
+  T* out = grad + row * p.ldo;
+  zero_span(out - s, valid ? end : s, s + (int)p.ldo, lane, 32, p.same != 0);
+  if (!valid) {
+    if (lane == 0) p.rows[row] = 0.f;
+    return;
+  }
+  // ---- maximum, sums
+  float m = ez != ez ? -INFINITY : ez;
+#pragma unroll
+  for (int i = 0; i < NVR; ++i)
+    if constexpr (W == 8) {
+      const __nv_bfloat162* h2 = reinterpret_cast<const __nv_bfloat162*>(&raw[i].raw);
+      const __nv_bfloat162 m2 = __hmax2(__hmax2(h2[0], h2[1]), __hmax2(h2[2], h2[3]));
+      m = fmaxf(m, fmaxf(__low2float(m2), __high2float(m2)));
+    } else {
+#pragma unroll
+      for (int c = 0; c < W; ++c) m = fmaxf(m, raw[i].get(c));
+    }
+  m = warp_max_redux(m);
+  const float base = m == -INFINITY ? 0.f : m;
+  const uint64_t cT2 = tc::pack2(p.cT, p.cT), c12 = tc::pack2(p.c1, p.c1);
+  const uint64_t neg2 = tc::pack2(-base, -base);
+  uint64_t sT2 = 0ull, s12 = 0ull;
+#pragma unroll
+  for (int i = 0; i < NVR; ++i)
+#pragma unroll
+    for (int c = 0; c < W / 2; ++c) add_exps<MODE>(tc::add2(pair_of(raw[i], c), neg2), c, cT2, c12, sT2, s12);
+  float sT, s1;
+  {
+    add_exps<MODE>(tc::pack2(ez - base, -INFINITY), 0, cT2, c12, sT2, s12);
+    float a, c;
+    tc::unpack2(sT2, a, c); sT = warp_sum(a + c);
+    tc::unpack2(s12, a, c); s1 = MODE == EXP_ONE ? sT : warp_sum(a + c);
+  }
+  // ---- the teacher's distribution, the divergence and the row's loss
+  const Teacher te = teacher_of(idx, q, p, lane);
+  const float wkT = te.some ? p.wk * p.temp : 0.f, log_sT = logf(sT);
+  float kl = 0.f;
+  for (int j = lane; j < k; j += 32)
+    if (q[j] != 0.f) kl += q[j] * fmaf(p.temp, ((p.t[row * k + j] - te.top) * p.inv_t - te.lts) + log_sT, base - zt[j]);     // T times the divergence
+  kl = warp_sum(kl);
+  if (lane == 0) {
+    float r = wkT != 0.f ? p.wk * p.temp * kl : 0.f;
+    if (p.wc != 0.f) r += p.wc * (logf(s1) - (zy - base));
+    p.rows[row] = r;
+  }
+  // ---- gradient
+  const float f1 = MODE == EXP_ONE ? (p.wc + wkT) / s1 * inv_n : p.wc / s1 * inv_n, fT = MODE == EXP_ONE ? 0.f : wkT / sT * inv_n;
+  const uint64_t f12 = tc::pack2(f1, f1), fT2 = tc::pack2(fT, fT);
+  __syncwarp();                            // every lane has read what it needs of the row: the gradient may lie over it
+#pragma unroll
+  for (int i = 0; i < NVR; ++i) {
+    const int v = v0 + i * 32 + lane;
+    if (v < v1) {
+      // formed from the logits again: the compiler would keep converted logits or exponentials, twice the registers
+      uint32_t* w = reinterpret_cast<uint32_t*>(&raw[i].raw);
+      asm volatile("" : "+r"(w[0]), "+r"(w[1]), "+r"(w[2]), "+r"(w[3]));
+      const Vec16<T> o = slopes_of<MODE>(raw[i], neg2, cT2, c12, f12, fT2);
+      T* at = out + v * W - s;
+      if (p.same) o.store(at);
+      else
+#pragma unroll
+        for (int c = 0; c < W; ++c) at[c] = reinterpret_cast<const T*>(&o.raw)[c];
+    }
+  }
+  if (has_edge) out[ec] = from_f<T>(slope<MODE>(ez - base, p.cT, p.c1, f1, fT));
+  __syncwarp();                            // the tables, and the targets' first values
+  targets<MODE>(out, Slope{base, f1, fT, wkT * inv_n, p.wc * inv_n}, p, lane, 32, idx, q, zt, y, zy);
+}
+
+// One block each: eight elements per thread under way at a time, added up in an order of their own.
+constexpr int TALLY = 1024, TALLY_EACH = 8;
+__global__ void __launch_bounds__(TALLY) distill_count_kernel(const int32_t* __restrict__ labels, int M, int V, int* __restrict__ n_valid) {
   overlap_sync();
   __shared__ int sh[32];
   int c = 0;
-  for (int i = threadIdx.x; i < M; i += blockDim.x) c += (labels[i] >= 0 && labels[i] < V) ? 1 : 0;
+  for (int i0 = threadIdx.x; i0 < M; i0 += TALLY * TALLY_EACH) {
+    int y[TALLY_EACH];
+#pragma unroll
+    for (int e = 0; e < TALLY_EACH; ++e) y[e] = i0 + e * TALLY < M ? labels[i0 + e * TALLY] : -1;
+#pragma unroll
+    for (int e = 0; e < TALLY_EACH; ++e) c += y[e] >= 0 && y[e] < V ? 1 : 0;
+  }
   c = __reduce_add_sync(0xffffffffu, c);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = c;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < (int)(blockDim.x >> 5); ++w) c += sh[w];
-    *n_valid = c;
+  if (threadIdx.x < 32) {
+    c = __reduce_add_sync(0xffffffffu, sh[threadIdx.x]);
+    if (threadIdx.x == 0) *n_valid = c;
   }
 }
 
-__global__ void distill_loss_kernel(const float* __restrict__ rows, int M, const int* __restrict__ n_valid, int n_fixed, float* __restrict__ loss) {
+__global__ void __launch_bounds__(TALLY) distill_loss_kernel(const float* __restrict__ rows, int M, const int* __restrict__ n_valid, int n_fixed, float* __restrict__ loss) {
   overlap_sync();
   __shared__ double sh[32];
   double s = 0.0;
-  for (int i = threadIdx.x; i < M; i += blockDim.x) s += (double)rows[i];
+  for (int i0 = threadIdx.x; i0 < M; i0 += TALLY * TALLY_EACH) {
+    float r[TALLY_EACH];
+#pragma unroll
+    for (int e = 0; e < TALLY_EACH; ++e) r[e] = i0 + e * TALLY < M ? rows[i0 + e * TALLY] : 0.f;
+#pragma unroll
+    for (int e = 0; e < TALLY_EACH; ++e) s += (double)r[e];
+  }
   for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
   if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < (int)(blockDim.x >> 5); ++w) s += sh[w];
+  if (threadIdx.x < 32) {
+    s = sh[threadIdx.x];
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
     const int n = n_valid ? *n_valid : n_fixed;
-    *loss = n > 0 ? (float)(s / n) : 0.f;
+    if (threadIdx.x == 0) *loss = n > 0 ? (float)(s / n) : 0.f;
   }
 }
 
@@ -677,6 +853,19 @@ cudaError_t launch_ring(const T* logits, T* grad, const DistillArgs& p, int M, i
   }
   const int64_t most = (int64_t)num_sms() * (fit < MINB ? fit : MINB);
   return launch_overlapped(kernel, dim3((unsigned)(M < most ? M : most)), dim3(THREADS), (size_t)nbuf * buf + tables, st, logits, grad, p, M, nbuf, buf, status);
+}
+
+// Rows of up to 8 vectors per lane of a warp.  Warps and rings, bf16 at T 2: 16384 x 128 28 and 55 us, 8192 x 1000 18.6 and 36, 8192 x
+// 2000 25 and 41; with 16 vectors 8192 x 4000 49 and 52, but 64 x 4000 11.3 and 10.3.
+constexpr int WARP_MOST = 8 * 32;
+template <typename T, int MODE>
+cudaError_t warp_rows(const T* logits, T* grad, const DistillArgs& p, int M, cudaStream_t st) {
+  const int nv = p.V / Vec16<T>::N;
+  auto go = [&](auto kernel) -> cudaError_t {
+    return launch_overlapped(kernel, dim3((unsigned)((M + (int64_t)WARP_ROWS - 1) / WARP_ROWS)), dim3(32 * WARP_ROWS), (size_t)WARP_ROWS * 3 * ((p.k + 3) / 4 * 4) * 4, st,
+                             logits, grad, p, M);
+  };
+  return nv <= 4 * 32 ? go(distill_warp_kernel<T, 4, MODE>) : go(distill_warp_kernel<T, 8, MODE>);
 }
 
 int ring_buffer(int V, size_t es) { return (int)(((size_t)V * es + 15) / 16 * 16 + 16); }         // a row at any alignment
@@ -714,10 +903,10 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
   cudaError_t e = cudaSuccess;
   const size_t es = dtype_size(dt);
   p.same = ((reinterpret_cast<uintptr_t>(logits) - reinterpret_cast<uintptr_t>(grad)) & 15u) == 0 && ((ld - ldo) * (int64_t)es) % 16 == 0;
-  const bool in_ring = ring_supported(V, k, es);
+  const bool in_warp = V * (int64_t)es / 16 <= WARP_MOST, in_ring = ring_supported(V, k, es);
   p.count_here = in_ring && count && M <= COUNT_HERE;
   if (count && !p.count_here) {
-    e = launch_overlapped(distill_count_kernel, dim3(1), dim3(1024), 0, st, labels, M, V, n_valid);
+    e = launch_overlapped(distill_count_kernel, dim3(1), dim3(TALLY), 0, st, labels, M, V, n_valid);
     if (e != cudaSuccess) return e;
   }
   auto run = [&](auto type) -> cudaError_t {
@@ -726,10 +915,14 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
     const T* z = (const T*)logits;
     T* g = (T*)grad;
     if (in_ring) {
-      if (!two) return ring<T, EXP_ONE>(z, g, p, M, status, st);
-      if (temperature == 2.0f) return ring<T, 2>(z, g, p, M, status, st);
-      if (temperature == 3.0f) return ring<T, 3>(z, g, p, M, status, st);
-      return temperature == 4.0f ? ring<T, 4>(z, g, p, M, status, st) : ring<T, EXP_TWO>(z, g, p, M, status, st);
+      auto held = [&](auto mode) -> cudaError_t {
+        return in_warp ? warp_rows<T, mode>(z, g, p, M, st) : ring<T, mode>(z, g, p, M, status, st);
+      };
+      if (!two) return held(std::integral_constant<int, EXP_ONE>());
+      if (temperature == 2.0f) return held(std::integral_constant<int, 2>());
+      if (temperature == 3.0f) return held(std::integral_constant<int, 3>());
+      if (temperature == 4.0f) return held(std::integral_constant<int, 4>());
+      return held(std::integral_constant<int, EXP_TWO>());
     }
     const bool vec = ld % N == 0 && ldo % N == 0 && ((reinterpret_cast<uintptr_t>(logits) | reinterpret_cast<uintptr_t>(grad)) & 15u) == 0;
     auto go = [&](auto kernel) -> cudaError_t { return launch_overlapped(kernel, dim3((unsigned)M), dim3(256), 0, st, z, g, p); };
@@ -738,7 +931,7 @@ cudaError_t distill(int dt, const void* logits, int64_t ld, const int32_t* label
   };
   e = dt == DT_BF16 ? run(bf16()) : run(float());
   if (e != cudaSuccess) return e;
-  return launch_overlapped(distill_loss_kernel, dim3(1), dim3(1024), 0, st, (const float*)rows, M, (const int*)p.n_valid, p.n_fixed, loss);
+  return launch_overlapped(distill_loss_kernel, dim3(1), dim3(TALLY), 0, st, (const float*)rows, M, (const int*)p.n_valid, p.n_fixed, loss);
 }
 
 }  // namespace sl

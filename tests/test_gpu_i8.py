@@ -509,6 +509,22 @@ def test_distill_loss_of_masked_and_broken_logits_at_every_column(V, T, dtype):
     check(rows[ok], rr, rel * (rr.abs() + 0.5 + 0.5 * T * T * 50), "rows")
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("V", [1, 3, 8, 9, 15, 255, 256, 1023, 1024, 1025, 1031, 2047, 2048, 2056, 2063, 4103])
+def test_distill_loss_around_the_widths_that_change_the_kernel(V, dtype):
+    """Widths around those that a warp, its variants and a block hold, rows at every place of a vector, more rows than a block's eight."""
+    z, idx, t, y = distill_case(13, V, min(V, 9), dtype, V + 3)
+    for T in (1.0, 2.0, 1.3):
+        for by in (0, 1):
+            zz = offset(z, by)
+            got = B.distill_loss(zz, idx, t, labels=y, temperature=T, ce_weight=0.4, kd_weight=0.6)
+            check_distill(z, idx, t, y, T, 0.4, 0.6, got)
+            same = offset(z, by)
+            B.distill_loss(same, idx, t, labels=y, temperature=T, ce_weight=0.4, kd_weight=0.6, dlogits=same)
+            assert by and V > 1 or torch.equal(same, got[2])
+            check_distill(z, idx, t, y, T, 0.4, 0.6, (got[0], got[1], same))
+
+
 @pytest.mark.parametrize("M", [300, 5000])
 def test_distill_loss_of_many_rows(M):
     """More rows than blocks, and than a block looks at together; many that take no part, first and last among them."""
