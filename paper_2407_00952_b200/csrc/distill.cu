@@ -513,7 +513,7 @@ distill_ring_kernel(const T* logits, T* grad, DistillArgs p, int M, int nbuf, in
       const int row = sh_rows[at], y = sh_ys[at], slot = at % SLOTS, par = at & 1, b = used % nbuf, s = shift_of(row);
       T* out = grad + row * p.ldo - s;     // position q = s + column
       const int end = s + V, nvec = (end + W - 1) / W, last = nvec - 1;
-      tc::mbar_wait(tc::smem_u32(&bars[b]), (uint32_t)(used / nbuf) & 1u, &sh_abort, status, 81);
+      const bool arrived = tc::mbar_wait(tc::smem_u32(&bars[b]), (uint32_t)(used / nbuf) & 1u, &sh_abort, status, 81);
       T* zs = reinterpret_cast<T*>(smem + (size_t)b * buf_bytes);
       // A ragged first or last vector (in the first and last row of all the copies left it out): the thread that owns it keeps its
       // logits for the gradient and puts -inf around them.
@@ -581,7 +581,15 @@ distill_ring_kernel(const T* logits, T* grad, DistillArgs p, int M, int nbuf, in
         sh_m[par][warp] = wm; sh_sT[par][warp] = sT;
         if constexpr (MODE != EXP_ONE) sh_s1[par][warp] = s1;
       }
-      __syncthreads();
+      if (__syncthreads_or(!arrived)) {
+        // A row that did not arrive: `status` holds the code, neither this row nor a later one of the block is written, no copy follows.
+        // Those under way (this row's; before the first row's barrier the second row's too) land, or 2 ms pass, before the shared
+        // memory becomes another block's.
+        auto landed = [&](int u) { return tc::mbar_test(tc::smem_u32(&bars[u % nbuf]), (uint32_t)(u / nbuf) & 1u); };
+        const bool second = nbuf > 1 && at == 0 && count > 1;
+        for (int i = 0; i < 2000 && !(landed(used) && (!second || landed(used + 1))); ++i) __nanosleep(1000);
+        return;
+      }
       if (tid == ISSUER && nbuf > 1 && at > 0 && at + 1 < count) issue(sh_rows[at + 1], (used + 1) % nbuf);    // nobody reads the previous row's logits any more
       float base;
       {

@@ -86,8 +86,8 @@ __device__ __forceinline__ unsigned long long global_ns() {
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
   return t;
 }
-// Bounded wait.  Returns false when the limit expired or another role of this CTA already gave up.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+// Bounded wait.  Returns false when the limit expired or another role of this CTA already gave up: what was waited for is then not there.
+[[nodiscard]] __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
   if (mbar_try(bar, parity)) return true;
   unsigned long long t0 = global_ns();
   uint32_t spins = 0;
@@ -122,7 +122,7 @@ __device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {
 }
 // mbar_wait for a whole converged warp, with a warp-uniform result.  Every lane polls: with one lane polling and the
 // result broadcast the wait of a lone CTA's issuer was 10 % longer per 64-deep block.
-__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
+[[nodiscard]] __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
   if (__all_sync(0xffffffffu, mbar_try(bar, parity))) return true;
   const unsigned long long t0 = global_ns();
   uint32_t spins = 0;
