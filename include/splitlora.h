@@ -402,6 +402,7 @@ int splitlora_linear_i8(int dtype, const int8_t* x, int64_t ld_x, const float* x
  *   row_loss[m] = ce_weight (-log softmax(z)[label]) + kd_weight T^2 sum_j q_j (log q_j - log softmax(z / T)[top_idx_j])
  *   loss        = sum_m row_loss[m] / n
  *   dlogits     = (ce_weight (softmax(z) - [label]) + kd_weight T (softmax(z / T) - q)) / n
+ * A term whose weight is 0 is left out, whatever its operands hold.
  * labels [M] or NULL (then ce_weight must be 0); a row whose label lies outside [0, vocab) takes no part: loss and gradient 0.  n
  * counts the rows that take part, or is `normalizer` where that is positive (a shard of a larger batch; cf.
  * splitlora_set_loss_normalizer).  A row without a teacher entry, or whose entries are all -inf, has the label's term alone.  An

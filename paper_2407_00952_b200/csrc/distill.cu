@@ -160,7 +160,7 @@ distill_kernel(const T* logits, T* grad, DistillArgs p) {
     tmax = tmax != tmax ? tmax : other != other ? other : fmaxf(tmax, other);
   }
   __syncthreads();
-  const bool some = tmax != -INFINITY;     // no entry, or none with any weight: the teacher says nothing about this row
+  const bool some = tmax != -INFINITY && p.wk != 0.f;      // else the teacher says nothing about this row
   // teacher: sum of exponentials, then q and the row's divergence
   float tsum = 0.f;
   for (int j = tid; j < k; j += nt) tsum += some ? expf((sh_q[j] - tmax) * inv_t) : 0.f;
@@ -185,7 +185,7 @@ distill_kernel(const T* logits, T* grad, DistillArgs p) {
   __syncthreads();
   kl = 0.f;
   for (int w = 0; w < nw; ++w) kl += sh_red[w];
-  const float wk = some && p.wk != 0.f ? p.wk : 0.f;
+  const float wk = some ? p.wk : 0.f;
   if (tid == 0) {
     float r = wk != 0.f ? wk * p.temp * kl : 0.f;
     if (p.wc != 0.f) r += p.wc * (log_s1 - (sh_zy - base));
