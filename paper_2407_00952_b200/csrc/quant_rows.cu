@@ -12,7 +12,8 @@
 // 8192 x 4096 bf16, and the time of the traffic alone at the chip's measured copy rate: quantize 18.6 us (15.4), dequantize 16.5
 // (15.4), norm with residual, h and codes 42.5 (35.9), with y too 51 (46.2), gradient 38.6 (30.8), with residual 50 (41.1), with
 // residual and gain gradient 67 (41.1).
-// An output may be one of the inputs where the call allows it: a thread writes only elements that it alone has read.
+// An output may be one of the inputs where the call allows it (h one of x and the residual, dx one of dy and the residual): a thread writes
+// only elements that it alone has read, and these pointers promise the compiler nothing (no __restrict__).
 // FRAME: rows that do not start on 16-byte boundaries (odd widths in contiguous rows).  A row is then the whole 16-byte vectors in
 // it, position q = column + shift, and the elements around them, which are taken one by one; the gain and the factors, which start
 // at column 0, are read as words and shifted, and the codes turn back to column 0 through shared memory.
@@ -511,8 +512,8 @@ dequantize_kernel(const int8_t* __restrict__ codes, int64_t ldc, const float* __
 
 template <typename T, int FRAME, bool RES>
 __global__ void __launch_bounds__(1024)
-rmsnorm_quantize_kernel(const T* __restrict__ x, const T* __restrict__ resid, const T* __restrict__ g, int64_t M, int d, int threads, float eps,
-                        T* __restrict__ h, T* __restrict__ y, int8_t* __restrict__ codes, int64_t ldc, int words, float* __restrict__ scales) {
+rmsnorm_quantize_kernel(const T* x, const T* resid, const T* __restrict__ g, int64_t M, int d, int threads, float eps,
+                        T* h, T* __restrict__ y, int8_t* __restrict__ codes, int64_t ldc, int words, float* __restrict__ scales) {
   overlap_sync();
   constexpr int W = Vec16<T>::N;
   extern __shared__ __align__(16) uint8_t smem[];        // FRAME: codes
@@ -618,8 +619,8 @@ rmsnorm_quantize_kernel(const T* __restrict__ x, const T* __restrict__ resid, co
 // its threads the same columns.
 template <typename T, int FRAME, bool DG, bool RES, int MAXT>
 __global__ void __launch_bounds__(MAXT)
-rmsnorm_bwd_kernel(const T* __restrict__ dy, const T* __restrict__ h, const T* __restrict__ g, const T* __restrict__ resid, int64_t M, int d, int threads,
-                   int stages, float eps, T* __restrict__ dx, float* __restrict__ partial) {
+rmsnorm_bwd_kernel(const T* dy, const T* __restrict__ h, const T* __restrict__ g, const T* resid, int64_t M, int d, int threads, int stages, float eps,
+                   T* dx, float* __restrict__ partial) {
   overlap_sync();
   constexpr int W = Vec16<T>::N;
   extern __shared__ __align__(16) uint8_t smem[];        // the feed's slots; in the end (DG) sums

@@ -12,6 +12,32 @@ U, HALF, CHAIN, DTYPES = I.U, I.HALF, I.CHAIN, I.DTYPES
 BF16, F32 = torch.bfloat16, torch.float32
 
 
+# ---- norm and its gradient ---------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("M,d", [(50, 136), (37, 1001), (9, 8192), (6, 16383)])
+def test_norm_and_gradient_in_place_wherever_arrays_start(M, d, residual, dtype):
+    """The sum over x or the residual, dx over dy or the residual: bit for bit what separate outputs get, at every pair of places."""
+    g = I.gen(M + 5 * d)
+    x, r, dy = (I.randn(g, M, d, dtype=dtype) for _ in range(3))
+    gain = (1 + 0.2 * I.randn(g, d)).to(dtype)
+    for ox, orr in [(0, 0), (1, 1), (0, 3), (2, 1)]:
+        def fresh():
+            return I.offset(x, ox), I.offset(r, orr) if residual else None
+        a, b = fresh()
+        want = B.rmsnorm_quantize(a, gain, residual=b, want_y=True, h=I.offset(x, ox))
+        for into in (0, 1) if residual else (0,):
+            a, b = fresh()
+            got = B.rmsnorm_quantize(a, gain, residual=b, want_y=True, h=(a, b)[into])
+            for i in range(4):
+                assert torch.equal(got[i], want[i]), (ox, orr, into, i)
+        up, res = I.offset(dy, ox), I.offset(r, orr) if residual else None
+        dx = B.rmsnorm_bwd(up, x, gain, resid=res)[0]
+        assert torch.equal(B.rmsnorm_bwd(up, x, gain, resid=res, dx=up)[0], dx)
+        if residual:
+            assert torch.equal(B.rmsnorm_bwd(I.offset(dy, ox), x, gain, resid=res, dx=res)[0], dx)
+
+
 # ---- loss --------------------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype,V", [(BF16, 500), (BF16, 20000), (BF16, 120001), (BF16, 120000), (F32, 500), (F32, 20000), (F32, 60000)])
 def test_loss_without_the_teachers_weight_does_not_see_its_logits(V, dtype):
