@@ -502,7 +502,14 @@ _ARGTYPES = {
 }
 _F32, _BF16, _I8, _I32 = torch.float32, torch.bfloat16, torch.int8, torch.int32
 _DTYPE_ID = {_F32: DTYPE_FP32, _BF16: DTYPE_BF16}
-_raw_stream = torch._C._cuda_getCurrentRawStream      # the current stream's handle without a Stream object (3 us)
+
+
+def _public_raw_stream(dev: int) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+# The current stream's handle without a Stream object (3 us), where this PyTorch has that name (a build without CUDA has not).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _public_raw_stream)
 
 
 def _refuse(what: str, t: torch.Tensor, dtype, shape, dev: int):

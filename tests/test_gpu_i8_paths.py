@@ -52,3 +52,18 @@ def test_loss_without_the_teachers_weight_does_not_see_its_logits(V, dtype):
         u[:, 3::2] = bad
         for a, b in zip(B.distill_loss(z, idx, u, **kw), want):
             assert torch.equal(a, b), bad
+
+
+# ---- streams -----------------------------------------------------------------------------------
+def test_the_current_stream_by_either_name(monkeypatch):
+    x = I.randn(I.gen(2), 40, 136, dtype=BF16)
+    want = B.quantize_rows(x)
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        dev = torch.cuda.current_device()
+        assert B._raw_stream(dev) == B._public_raw_stream(dev) == s.cuda_stream
+        monkeypatch.setattr(B, "_raw_stream", B._public_raw_stream)
+        got = B.quantize_rows(x)
+    s.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
