@@ -250,7 +250,8 @@ class SplitLoRA:
     def set_teacher(self, top_idx: Optional[torch.Tensor], top_logits: Optional[torch.Tensor] = None, temperature: float = 1.0,
                     ce_weight: float = 0.5, kd_weight: float = 0.5):
         """A teacher's top logits for the loss of the server step: top_idx int32 and top_logits fp32, [K, b, T, k] (None: back to
-        the cross-entropy); see splitlora_set_teacher.  The tensors are kept and read by every step until replaced."""
+        the cross-entropy); see splitlora_set_teacher.  The tensors are kept and read by every step until replaced; they may be replaced
+        and dropped while a step is under way."""
         k = 0
         if top_idx is not None:
             c = self.cfg
@@ -261,6 +262,10 @@ class SplitLoRA:
                     raise SplitLoraError(ERR_ARG, f"set_teacher: contiguous int32 and float32 tensors {shape} on {self.workspace.device}")
         self._check(self.lib.splitlora_set_teacher(self.ctx, _ptr(top_idx), _ptr(top_logits if top_idx is not None else None), k,
                                                    C.c_float(temperature), C.c_float(ce_weight), C.c_float(kd_weight)))
+        if top_idx is not None:
+            # steps under way read them on the context's stream: no other tensor may get their memory before, should they be replaced
+            top_idx.record_stream(self.stream)
+            top_logits.record_stream(self.stream)
         self.teacher = (top_idx, top_logits) if top_idx is not None else None
 
     # ---- sharding hooks ----
