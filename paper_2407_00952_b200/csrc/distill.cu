@@ -43,7 +43,7 @@ struct DistillArgs {
   float inv_t;
   float* rows; int* n_valid; int n_fixed;
   int same;                // rows of logits and gradient start at the same place of a 16-byte vector
-  int count_here;          // the ring kernel counts the labels and leaves the count in n_valid
+  int count_here;          // the kernel that holds the rows counts the labels and leaves the count in n_valid
 };
 
 // Running maximum and sums of exponentials relative to it.
@@ -250,7 +250,7 @@ distill_kernel(const T* logits, T* grad, DistillArgs p) {
 // first and last vector patched by the threads that own them; the copies take whole vectors inside the buffer and plain
 // loads the ragged ends of the first and last row.
 // Modes from 2 on: temperatures 1 and `mode` (2, 3 or 4): e^z is that power of e^(z / mode).
-enum { EXP_POWERS = 2, EXP_MOST = 4 };
+enum { EXP_POWERS = 2 };
 template <int MODE> __device__ __forceinline__ float power(float x) { return MODE == 2 ? x * x : MODE == 3 ? x * x * x : (x * x) * (x * x); }
 template <int MODE> __device__ __forceinline__ uint64_t power2(uint64_t x) {
   const uint64_t s = tc::mul2(x, x);
@@ -844,7 +844,7 @@ __global__ void __launch_bounds__(TALLY) distill_loss_kernel(const float* __rest
 
 namespace {
 
-// Rows up to this many labels are counted by every block of the ring kernel instead of a launch in front of it.
+// Up to this many labels are counted by every block of the warp and ring kernels instead of a launch in front of them.
 constexpr int COUNT_HERE = 4096;
 // Static shared memory of a block with what the system keeps per block, dynamic shared memory of a block, all of an SM's.
 constexpr int RING_STATIC = 4096, RING_BYTES = 229376, SM_BYTES = 233472;

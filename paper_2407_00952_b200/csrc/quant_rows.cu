@@ -131,8 +131,8 @@ struct Place {
   }
 };
 
-// Sums and maximum over the threads of a row.  With whole warps per row every thread of the block takes part, in step; two sets of
-// shared memory in turn make one barrier per call enough.
+// Sums and maximum over the threads of a row.  With whole warps per row every thread of the block takes part, in step; where a block walks
+// several rows, two sets of shared memory in turn make one barrier per call enough.
 struct RowShared { float sum[2][32]; uint32_t top[32]; };
 template <int NS, bool MAX> __device__ __forceinline__ void reduce_row(float* s, float& largest, const Place& at, RowShared* sh) {
   uint32_t top = MAX ? __float_as_uint(largest) : 0u;    // no negative values: the order of the bits, NaN above all
@@ -328,14 +328,13 @@ __device__ __forceinline__ void codes_out(const uint8_t* mine, int8_t* cr, int s
   } else {
     for (int c = at.t; c < d; c += at.n) cr[c] = (int8_t)mine[s + c];
   }
-  if (at.n <= 32) __syncwarp();            // before the next row's codes (whole warps: its reduction's barrier)
 }
 // Shared memory of a row's codes, for `threads` threads.
 template <typename T> __host__ __device__ constexpr int code_bytes(int threads, int nv = NV) { return (threads * nv * Vec16<T>::N + 4 * Vec16<T>::N + 31) / 16 * 16; }
 __device__ __forceinline__ uint8_t one_code(float v, const RowScale& rs) { return rs.live ? (uint8_t)code_bits(v, rs.inv) : (uint8_t)0; }
 
-// The rows of a thread: its group's, every (groups of the grid)-th; only the gain's gradient is launched with fewer groups than
-// rows.  `lead`: the row of the block's first group, by which all its threads go through the same number of rows.
+// The rows of a thread that adds up over rows (the gain's gradient): its group's, every (groups of the grid)-th.  `lead`: the row of the
+// block's first group, by which all its threads go through the same number of rows.
 struct Walk {
   int64_t row, lead, step;
   __device__ __forceinline__ explicit Walk(const Place& at) {
@@ -517,7 +516,7 @@ rmsnorm_quantize_kernel(const T* x, const T* resid, const T* __restrict__ g, int
   overlap_sync();
   constexpr int W = Vec16<T>::N;
   extern __shared__ __align__(16) uint8_t smem[];        // FRAME: codes
-  __shared__ RowShared sh[2];
+  __shared__ RowShared sh;
   const Place at(threads);
   Feed<T, FRAME, RES ? 2 : 1, false> feed(0, smem);
   feed.array(0, x);
@@ -525,90 +524,85 @@ rmsnorm_quantize_kernel(const T* x, const T* resid, const T* __restrict__ g, int
   uint8_t* mine = smem + (size_t)at.group * code_bytes<T>(at.n);
   const bool fit_h = ((reinterpret_cast<uintptr_t>(h) - reinterpret_cast<uintptr_t>(x)) & 15u) == 0;
   const bool fit_y = ((reinterpret_cast<uintptr_t>(y) - reinterpret_cast<uintptr_t>(x)) & 15u) == 0;
-  Walk w(at);
-  feed.start(w.row, M, d, at);
-  for (int flip = 0; w.lead < M; w.row += w.step, w.lead += w.step, flip ^= 1) {
-    const bool in = w.row < M;
-    const int64_t row0 = (in ? w.row : 0) * d;
-    const Span<T, FRAME> f(x + row0, d);
-    const int v1 = in ? f.v1 : 0, ec = f.edge(at.t);
-    const bool has_edge = FRAME && in && at.t < f.edges;
-    feed.begin(w.row, w.row + w.step, M, d, at);
-    uint64_t sum2 = 0ull;
-    float es = 0.f, ev = 0.f, top = 0.f;
-    // x + residual, from the vectors as they came: formed twice, which costs less than the registers that would keep it
-    auto sum_of = [&](int k) {
-      Pairs<T> s = pairs_of(feed.raw[0][k]);
-      if constexpr (RES) {
-        const Pairs<T> rp = pairs_of(feed.raw[1][k]);
+  const bool in = at.row < M;              // lanes of a row past the last still take part in the warp's exchanges
+  const int64_t row0 = (in ? at.row : 0) * d;
+  const Span<T, FRAME> f(x + row0, d);
+  const int v1 = in ? f.v1 : 0, ec = f.edge(at.t);
+  const bool has_edge = FRAME && in && at.t < f.edges;
+  feed.begin(at.row, M, M, d, at);
+  uint64_t sum2 = 0ull;
+  float es = 0.f, ev = 0.f, top = 0.f;
+  // x + residual, from the vectors as they came: formed twice, which costs less than the registers that would keep it
+  auto sum_of = [&](int k) {
+    Pairs<T> s = pairs_of(feed.raw[0][k]);
+    if constexpr (RES) {
+      const Pairs<T> rp = pairs_of(feed.raw[1][k]);
 #pragma unroll
-        for (int i = 0; i < W / 2; ++i) s.v[i] = add2(s.v[i], rp.v[i]);
+      for (int i = 0; i < W / 2; ++i) s.v[i] = add2(s.v[i], rp.v[i]);
+    }
+    return s;
+  };
+#pragma unroll
+  for (int k = 0; k < NV; ++k) {
+    const int v = f.v0 + k * at.n + at.t;
+    if (v < v1) {
+      Vec16<T> gv;
+      load_gain<T, FRAME>(gv, g, f, v);
+      const Pairs<T> s = sum_of(k), gain = pairs_of(gv);
+#pragma unroll
+      for (int i = 0; i < W / 2; ++i) {
+        sum2 = fma2(s.v[i], s.v[i], sum2);
+        top = max_abs(top, mul2(s.v[i], gain.v[i]));
       }
-      return s;
-    };
+      if (h) store_row<T, FRAME>(h + row0, f, v, fit_h, s);
+    }
+  }
+  float sum;
+  {
+    float a, b;
+    unpack2(sum2, a, b);
+    sum = a + b;
+  }
+  if (has_edge) {
+    es = to_f<T>(feed.edge[0]);
+    if constexpr (RES) es = __fadd_rn(es, to_f<T>(feed.edge[1]));
+    ev = __fmul_rn(es, to_f<T>(g[ec]));
+    sum = fmaf(es, es, sum);
+    top = max_abs(top, ev);
+    if (h) h[row0 + ec] = from_f<T>(es);
+  }
+  reduce_row<1, true>(&sum, top, at, &sh);
+  const float rstd = rsqrtf(sum / d + eps);
+  const RowScale rs = row_scale(top, rstd);
+  if (at.t == 0 && in) scales[at.row] = rs.scale;
+  int8_t* cr = codes + at.row * ldc;
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int v = f.v0 + k * at.n + at.t;
-      if (v < v1) {
-        Vec16<T> gv;
-        load_gain<T, FRAME>(gv, g, f, v);
-        const Pairs<T> s = sum_of(k), gain = pairs_of(gv);
+  for (int k = 0; k < NV; ++k) {
+    const int v = f.v0 + k * at.n + at.t;
+    if (v < v1) {
+      Vec16<T> gv;
+      load_gain<T, FRAME>(gv, g, f, v);
+      Pairs<T> o = sum_of(k);
+      const Pairs<T> gain = pairs_of(gv);
 #pragma unroll
-        for (int i = 0; i < W / 2; ++i) {
-          sum2 = fma2(s.v[i], s.v[i], sum2);
-          top = max_abs(top, mul2(s.v[i], gain.v[i]));
-        }
-        if (h) store_row<T, FRAME>(h + row0, f, v, fit_h, s);
+      for (int i = 0; i < W / 2; ++i) o.v[i] = mul2(o.v[i], gain.v[i]);
+      uint32_t q[W / 4];
+      code_words<T>(q, o, rs.inv, rs.live);
+      store_words<W>(FRAME ? (void*)(mine + v * W) : (void*)(cr + v * W), q);
+      if (y) {
+        const uint64_t rstd2 = pack2(rstd, rstd);
+#pragma unroll
+        for (int i = 0; i < W / 2; ++i) o.v[i] = mul2(o.v[i], rstd2);
+        store_row<T, FRAME>(y + row0, f, v, fit_y, o);
       }
     }
-    float sum;
-    {
-      float a, b;
-      unpack2(sum2, a, b);
-      sum = a + b;
-    }
+  }
+  if constexpr (FRAME) {
     if (has_edge) {
-      es = to_f<T>(feed.edge[0]);
-      if constexpr (RES) es = __fadd_rn(es, to_f<T>(feed.edge[1]));
-      ev = __fmul_rn(es, to_f<T>(g[ec]));
-      sum = fmaf(es, es, sum);
-      top = max_abs(top, ev);
-      if (h) h[row0 + ec] = from_f<T>(es);
+      mine[f.s + ec] = one_code(ev, rs);
+      if (y) y[row0 + ec] = from_f<T>(ev * rstd);
     }
-    reduce_row<1, true>(&sum, top, at, &sh[flip]);
-    const float rstd = rsqrtf(sum / d + eps);
-    const RowScale rs = row_scale(top, rstd);
-    if (at.t == 0 && in) scales[w.row] = rs.scale;
-    int8_t* cr = codes + w.row * ldc;
-#pragma unroll
-    for (int k = 0; k < NV; ++k) {
-      const int v = f.v0 + k * at.n + at.t;
-      if (v < v1) {
-        Vec16<T> gv;
-        load_gain<T, FRAME>(gv, g, f, v);
-        Pairs<T> o = sum_of(k);
-        const Pairs<T> gain = pairs_of(gv);
-#pragma unroll
-        for (int i = 0; i < W / 2; ++i) o.v[i] = mul2(o.v[i], gain.v[i]);
-        uint32_t q[W / 4];
-        code_words<T>(q, o, rs.inv, rs.live);
-        store_words<W>(FRAME ? (void*)(mine + v * W) : (void*)(cr + v * W), q);
-        if (y) {
-          const uint64_t rstd2 = pack2(rstd, rstd);
-#pragma unroll
-          for (int i = 0; i < W / 2; ++i) o.v[i] = mul2(o.v[i], rstd2);
-          store_row<T, FRAME>(y + row0, f, v, fit_y, o);
-        }
-      }
-    }
-    if constexpr (FRAME) {
-      if (has_edge) {
-        mine[f.s + ec] = one_code(ev, rs);
-        if (y) y[row0 + ec] = from_f<T>(ev * rstd);
-      }
-      codes_out(mine, cr, f.s, in ? d : 0, at, words != 0);
-    }
-    feed.end(w.row + w.step, M, d, at);
+    codes_out(mine, cr, f.s, in ? d : 0, at, words != 0);
   }
 }
 
@@ -730,6 +724,7 @@ rmsnorm_bwd_kernel(const T* dy, const T* __restrict__ h, const T* __restrict__ g
       else dx[row0 + ec] = from_f<T>(__fmul_rn(rstd, t));
       if constexpr (DG) acc_edge = fmaf(ed, __fmul_rn(eh, rstd), acc_edge);
     }
+    if constexpr (!DG) break;              // a group per row
     feed.end(w.row + w.step, M, d, at);
   }
   feed.finish();
