@@ -493,7 +493,7 @@ def attention_bwd_static(qkv, o, lse, d_o, nseq, T, n_head, use_tensor_cores=Tru
 
 # ---- adapters over a frozen weight held in 8 bits --------------------------------------------
 # These calls are short enough (4-10 us on the device) for the host's share to count: argument types are declared once, so that
-# plain integers pass, and a tensor is checked in four comparisons (calls of 16-22 us -> 8-11).
+# plain integers pass, and a tensor is checked in four comparisons (calls of 16-22 us -> 8-16, the loss the longest).
 ERR_ARG, ERR_ALIGN = -1, -2
 _P, _I, _L, _F, _Z = C.c_void_p, C.c_int, C.c_int64, C.c_float, C.c_size_t
 _ARGTYPES = {

@@ -59,7 +59,8 @@ template <int MODE> __device__ __forceinline__ void online_merge(Online& a, cons
 
 // Rows wider than shared memory, one block each: a pass for the maximum and the running sums of exponentials, a pass that writes the
 // gradient from the logits' second read (L1 or L2).  4 exponentials per logit with two temperatures: bound by the exponential unit and
-// instruction issue as much as by traffic (it took 467 us where the ring kernel takes 174).
+// instruction issue as much as by traffic: 1024 x 128256 bf16 at T 2 182 us, where the traffic takes 80 (4096 x 50257 took 467 us with it,
+// where the ring kernel takes 173).
 template <typename T, int W, int MODE>
 __global__ void __launch_bounds__(512)
 distill_kernel(const T* logits, T* grad, DistillArgs p) {

@@ -755,7 +755,11 @@ template <typename TO, bool VEC, int S> cudaError_t launch_split(const I8Args& a
   return cudaLaunchKernelEx(&cfg, gemm_i8_split_kernel<TO, VEC, S>, mX, mW, mY, p);
 }
 
-// The kernel with the least estimated time (ns): a fixed part, the time of a 128-deep block, rounds over the chip.
+// The kernel with the least estimated time (ns): a fixed part, the time of a 128-deep block, rounds over the chip.  Each kernel was timed
+// on 19 shapes (8 to 8192 tokens, 768 to 65536 deep), without and with a residual and with fp32 output: the one picked took at most 9 % more
+// than the fastest.  Examples, us (pairs 256 and 128 wide, clusters of 1, 2, 4, 8): 16 x 4096 -> 4096 -, -, 9.4, 7.2, 11.1, 20.4;
+// 256 x 4096 -> 4096 15.0, 10.0, 9.9, 14.4, 23.6, 46.0; 300 x 65536 -> 256 144, 79, 95, 49, 27, 16.7; 4096 x 4096 -> 11008 116, 133, 364 ...
+// The epilogue is not in the estimate: with a residual 4096 x 1024 -> 1024 takes 10.5 in the 256-wide tiles it gets, 9.8 in the others.
 enum Pick { PICK_PAIR256, PICK_PAIR128, PICK_SPLIT1, PICK_SPLIT2, PICK_SPLIT4, PICK_SPLIT8 };
 Pick pick(const I8Args& a) {
   const int dev = current_device();

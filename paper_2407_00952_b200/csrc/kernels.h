@@ -248,6 +248,8 @@ cudaError_t dequantize_rows(int dt, const int8_t* codes, int64_t ldc, const floa
 cudaError_t rmsnorm_quantize(int dt, const void* x, const void* resid, const void* g, int64_t M, int d, float eps, void* h, void* y, int8_t* codes,
                              int64_t ldc, float* scales, cudaStream_t st);
 // dx = resid + d/dh (resid may be null); dg (may be null) fp32 [d] with partial of at least rmsnorm_dg_scratch_floats.
+// DG_PARTIAL_ROWS: the most blocks, each of which leaves a row of partial sums; a device with fewer SMs launches one block per SM and leaves
+// the rest of the scratch alone (its size is the same on every device).
 constexpr int DG_PARTIAL_ROWS = 592;
 size_t rmsnorm_dg_scratch_floats(int64_t M, int d);
 cudaError_t rmsnorm_gain_bwd(int dt, const void* dy, const void* h, const void* g, const void* resid, int64_t M, int d, float eps, void* dx, float* dg,

@@ -10,8 +10,8 @@
 // lanes per row where a warp holds it, else whole warps, up to 1024 threads), so it is read once.  Rows are many and short-lived: a
 // block each (walking the rows with copies one row ahead was 10-20 % slower where no sums are carried from row to row).
 // 8192 x 4096 bf16, and the time of the traffic alone at the chip's measured copy rate: quantize 18.6 us (15.4), dequantize 16.5
-// (15.4), norm with residual, h and codes 42.5 (35.9), with y too 51 (46.2), gradient 38.6 (30.8), with residual 50 (41.1), with
-// residual and gain gradient 67 (41.1).
+// (15.4), norm with residual, h and codes 41.3 (35.9), with y too 51 (46.2), gradient 35.2 (30.8), with residual 45.3 (41.1), with
+// residual and gain gradient 66 (41.1).
 // An output may be one of the inputs where the call allows it (h one of x and the residual, dx one of dy and the residual): a thread writes
 // only elements that it alone has read, and these pointers promise the compiler nothing (no __restrict__).
 // FRAME: rows that do not start on 16-byte boundaries (odd widths in contiguous rows).  A row is then the whole 16-byte vectors in
