@@ -64,7 +64,7 @@ def test_a_teacher_replaced_while_its_step_is_under_way():
     g = torch.Generator(device="cuda").manual_seed(3)
 
     def teacher():
-        return (torch.randint(0, w.vocab, shape, device="cuda", generator=g, dtype=torch.int32), 4 + 2 * torch.randn(shape, device="cuda", generator=g))
+        return (torch.randint(0, w.vocab, shape, device="cuda", generator=g, dtype=torch.int32), 4 + 2 * torch.randn(shape, device="cuda", generator=g, dtype=torch.float32))
 
     side = torch.cuda.Stream()
     with torch.cuda.stream(side):
