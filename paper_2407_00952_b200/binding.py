@@ -256,6 +256,8 @@ class SplitLoRA:
         if top_idx is not None:
             c = self.cfg
             k = int(top_idx.shape[-1])
+            if k >> 31:
+                _past_32_bits("set_teacher")
             shape = (c.n_clients, c.batch_per_client, c.seq, k)
             for t, dt in ((top_idx, torch.int32), (top_logits, torch.float32)):
                 if t is None or t.dtype != dt or tuple(t.shape) != shape or t.device != self.workspace.device or not t.is_contiguous():
@@ -527,6 +529,11 @@ def _refuse(what: str, t: torch.Tensor, dtype, shape, dev: int):
     raise SplitLoraError(ERR_ARG, f"{what}: {why}")
 
 
+def _past_32_bits(what: str):
+    # ctypes would pass the low 32 bits on, and the call answer for a part of the tensor
+    raise SplitLoraError(ERR_ARG, f"{what}: a size that is negative or beyond 2^31 - 1")
+
+
 def _in(what: str, t: Optional[torch.Tensor], dtype, shape, dev: int) -> int:
     """Address of a contiguous tensor (0 for None) once its type, shape and device are what the call takes."""
     if t is None:
@@ -555,6 +562,8 @@ def _matrix(what: str, x: torch.Tensor):
         raise SplitLoraError(ERR_ARG, f"{what}: {x.dtype} of {x.dim()} dimensions, not a float32 or bfloat16 matrix")
     dev = torch.cuda.current_device()
     M, d = x.shape
+    if d >> 31:
+        _past_32_bits(what)
     if x.get_device() != dev:
         _refuse(what, x, x.dtype, x.shape, dev)
     return dt, M, d, dev
@@ -677,6 +686,8 @@ def linear_i8(x: torch.Tensor, x_scales: torch.Tensor, W: torch.Tensor, w_scales
         raise SplitLoraError(ERR_ARG, "x and W are matrices of codes")
     M, K = x.shape
     N = W.shape[0]
+    if (M | N | K) >> 31:
+        _past_32_bits("linear_i8")
     if y is None:
         dt, dev = _DTYPE_ID.get(dtype), torch.cuda.current_device()
         if dt is None:
@@ -708,6 +719,9 @@ def distill_loss(logits: torch.Tensor, top_idx: torch.Tensor, top_logits: torch.
     if top_idx.dim() != 2:
         raise SplitLoraError(ERR_ARG, "top_idx is a matrix [M, k]")
     k = top_idx.shape[1]
+    V = ld if vocab is None else int(vocab)
+    if (M | V | k | normalizer) >> 31:
+        _past_32_bits("distill_loss")
     t = logits.dtype
     zp = _in("logits", logits, t, (M, ld), dev)
     dlogits, dp = _like_out("dlogits", dlogits, logits, (M, ld), dev)
@@ -715,7 +729,7 @@ def distill_loss(logits: torch.Tensor, top_idx: torch.Tensor, top_logits: torch.
     p = out.data_ptr()
     rc = load().splitlora_distill_loss(
         dt, zp, ld, 0 if labels is None else _in("labels", labels, _I32, (M,), dev), _in("top_idx", top_idx, _I32, (M, k), dev),
-        _in("top_logits", top_logits, _F32, (M, k), dev), M, ld if vocab is None else int(vocab), k, temperature, ce_weight, kd_weight, normalizer,
+        _in("top_logits", top_logits, _F32, (M, k), dev), M, V, k, temperature, ce_weight, kd_weight, normalizer,
         dp, ld, p, p + 4 * M, p + 4 * M + 4, _raw_stream(dev))
     if rc:
         _rc(rc, "distill_loss")
